@@ -320,7 +320,8 @@ T5_API int t5_attention_backward_onepass(
     int64_t ds_scratch_bytes, void* stream);
 
 /* Status word for the kernel-level entry points (t5_attention,
- * t5_attention_backward_onepass, t5_attention_backward_noalloc, t5_gemm): they
+ * t5_attention_backward_onepass, t5_attention_backward_noalloc, t5_gemm, and the
+ * paged-cache calls with their codes 201 - 203): they
  * have no workspace whose first word could carry it.  d_status: device int32,
  * zeroed by the caller, or NULL to switch reporting off (the default).  A
  * tensor-core kernel whose bounded wait on a TMA / MMA barrier runs out writes
@@ -365,6 +366,76 @@ T5_API int t5_attention_backward_noalloc(
     const void* d_o, int32_t ldo, const float* d_o32, const float* d_lse, const int32_t* d_code_q,
     const int32_t* d_code_k, const float* d_bias_delta, const void* d_do, int32_t lddo, void* d_dq,
     int32_t lddq, void* d_dk, int32_t lddk, void* d_dv, int32_t lddv, float* d_dbias_delta, void* stream);
+
+/* ---- serving: a paged key / value cache ("Model Implementation" section: the inference method; the paper
+ *      describes no cache) ----
+ * Sequences of any length share two pools of pages (keys, values).  Element c of head g of a key lives at
+ *   d_k_pages[page * page_stride + slot * slot_stride + g * head_stride + c]      (strides in elements)
+ * and its value at the same place of d_v_pages, so [page, slot, head, c] and [page, head, slot, c] pools, or both
+ * kinds in one buffer, are a matter of strides.  Position j of sequence s is slot j % page_size of page
+ * d_page_table[s * ld_table + j / page_size].  Pages of a sequence lie in any order and may be shared by sequences.
+ *  - dtype 0 / 1 (float32 / bfloat16) is the type of the pools and of q, k, v, out; d_kv is 32, 64 or 128.
+ *  - Pools, q, k, v and outputs are 16-byte aligned, and so are all row, page, slot and head strides.
+ *  - max_pages * page_size <= 2^30 positions per sequence.
+ *  - What the host cannot check is checked on the device and reported through t5_kernel_status_word: 201 = a token to
+ *    append has no place (sequence, position or page out of range; it is left out), 202 = a page in front of a length is
+ *    out of range (its keys count as absent), 203 = a length beyond max_pages * page_size (cut to that). */
+
+/* Appends n_tokens new keys and values: token t, heads in columns [g * d_kv, (g + 1) * d_kv) of row t of d_k / d_v (row
+ * strides ldk, ldv), goes to position d_positions[t] of sequence d_seq[t] (0 .. n_seqs - 1).  A negative position is
+ * padding: nothing is written for it.  Two tokens of one call must not name the same slot (one of them would win).
+ * rot_dim > 0 (a multiple of 16, at most d_kv) first rotates the leading rot_dim columns of every key head by position:
+ *   (x0, x1) -> (x0 cos a - x1 sin a, x1 cos a + x0 sin a),  a = position * rot_base^(-2 i / rot_dim),
+ * pair i being columns (i, i + rot_dim / 2), or (2 i, 2 i + 1) when rot_interleaved is 1.  The angle is formed in
+ * float64.  rot_dim = 0 (the relative-bias models) copies.  d_q (NULL: none), n_heads heads, is rotated alike into
+ * d_q_out, which may be d_q itself; queries of padding are copied unrotated.  Slots that no token names keep what they
+ * hold. */
+T5_API int t5_paged_kv_append(int32_t dtype, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads, int32_t d_kv,
+                              const void* d_q, int64_t ldq, const void* d_k, int64_t ldk, const void* d_v, int64_t ldv,
+                              void* d_q_out, int64_t ldqo, const int32_t* d_seq, const int32_t* d_positions,
+                              int32_t rot_dim, double rot_base, int32_t rot_interleaved, void* d_k_pages,
+                              void* d_v_pages, int32_t n_pages, int32_t page_size, int64_t page_stride,
+                              int64_t slot_stride, int64_t head_stride, const int32_t* d_page_table, int32_t n_seqs,
+                              int32_t max_pages, int64_t ld_table, void* stream);
+
+/* Attention of new tokens over the cache.  Row r of d_q (n_rows rows, n_heads heads in columns) is a token of sequence
+ * r / n_q that sees the first d_lens[r] positions:
+ *   out[r, h] = sum_j softmax_j(scale q[r, h].k_j + d_bias[h * n_bias + max(n_bias - 1 - distance, 0)]) v_j,
+ *   distance = d_lens[r] - 1 - j,   lse[r, h] = log sum_j exp(...),
+ * with k, v from kv head h / (n_heads / n_kv_heads) of the pools.  n_q (1 .. 64) new tokens per sequence share one pass
+ * over its cache (a draft to be verified: lens L, L + 1, ...), each with its own length.  d_bias (NULL with n_bias = 0)
+ * is indexed like d_bias_delta of t5_attention with the far end saturating.  A row that sees no key (length <= 0, or a
+ * bias of -infinity on all of them) gives zero and lse -infinity.  What the cache holds behind a row's length does not
+ * enter its result.  d_lse [n_rows, n_heads] float32 may be NULL.  The result does not depend on
+ * the run: sums are cut by the lengths alone.
+ * d_workspace: t5_paged_attention_workspace_bytes(...) bytes, contents undefined before and after; calls that may
+ * overlap on the GPU need one each. */
+T5_API int t5_paged_attention_workspace_bytes(int32_t n_rows, int32_t n_q, int32_t n_heads, int32_t n_kv_heads,
+                                              int32_t d_kv, int64_t* bytes);
+T5_API int t5_paged_attention(int32_t dtype, int32_t n_rows, int32_t n_q, int32_t n_heads, int32_t n_kv_heads,
+                              int32_t d_kv, float scale, const void* d_q, int64_t ldq, const void* d_k_pages,
+                              const void* d_v_pages, int32_t n_pages, int32_t page_size, int64_t page_stride,
+                              int64_t slot_stride, int64_t head_stride, const int32_t* d_page_table, int32_t max_pages,
+                              int64_t ld_table, const int32_t* d_lens, const float* d_bias, int32_t n_bias, void* d_out,
+                              int64_t ldo, float* d_lse, void* d_workspace, int64_t workspace_bytes, void* stream);
+
+/* Verification of drafted tokens from given random numbers.  Sequence s has n = d_n_draft[s] (NULL: max_draft) tokens
+ * x_i = d_draft_tokens[s * ld_draft_tokens + i]; target_i = row i of the target's probabilities (rows 0 .. n: at
+ * d_target + s * target_seq_stride + i * target_row_stride, vocab values), draft_i likewise (d_draft NULL: draft_i is one
+ * at x_i, the token was not drawn).  x_0, x_1, ... are accepted while u_i draft_i(x_i) < target_i(x_i) with
+ * u_i = d_u_accept[s * ld_u_accept + i] in [0, 1).  Behind the a accepted ones token y is drawn from
+ * r = max(target_a - draft_a, 0) if x_a was refused, from r = target_n if none was:  the first y with
+ * sum_{v <= y} r_v > d_u_sample[s] sum_v r_v, in float64.  Values that are not positive and finite count as 0; if that
+ * leaves nothing of a difference the token is drawn from target_a, and if that has nothing either it is -1.  A drafted
+ * token outside [0, vocab) is refused.
+ * Writes d_out_tokens[s * ld_out_tokens + 0 .. max_draft] = accepted tokens, y, then -1, and d_n_accepted[s] = a.
+ * dtype: of both probability arrays.  vocab <= 2^20, max_draft <= 1024 (0: plain sampling from target_0). */
+T5_API int t5_verify_draft(int32_t dtype, int32_t n_seqs, int32_t max_draft, int32_t vocab, const void* d_target,
+                           int64_t target_seq_stride, int64_t target_row_stride, const void* d_draft,
+                           int64_t draft_seq_stride, int64_t draft_row_stride, const int32_t* d_draft_tokens,
+                           int64_t ld_draft_tokens, const int32_t* d_n_draft, const float* d_u_accept,
+                           int64_t ld_u_accept, const float* d_u_sample, int32_t* d_out_tokens, int64_t ld_out_tokens,
+                           int32_t* d_n_accepted, void* stream);
 
 #ifdef __cplusplus
 }

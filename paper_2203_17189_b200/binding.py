@@ -55,7 +55,8 @@ EXPORTS = ["t5_create", "t5_destroy", "t5_last_error", "t5_param_count", "t5_par
            "t5_launch_count", "t5_relpos_buckets", "t5_xent_zloss",
            "t5_gemm", "t5_attention", "t5_attention_backward_noalloc",
            "t5_attention_ds_scratch_bytes", "t5_attention_backward_onepass",
-           "t5_kernel_status_word", "t5_selftest_bounded_wait", "t5_set_grad_hook"]
+           "t5_kernel_status_word", "t5_selftest_bounded_wait", "t5_set_grad_hook",
+           "t5_paged_kv_append", "t5_paged_attention_workspace_bytes", "t5_paged_attention", "t5_verify_draft"]
 
 _lib = None
 
@@ -111,6 +112,12 @@ def lib():
         L.t5_attention_ds_scratch_bytes.argtypes = [i32] * 4 + [C.POINTER(i64)]
         L.t5_attention_backward_onepass.argtypes = ([i32] * 6 + [f32] + [vp, i32] * 4 + [vp] * 5
                                                     + [vp, i32] * 4 + [vp, vp, i32, vp, i64, vp])
+        L.t5_paged_kv_append.argtypes = ([i32] * 5 + [vp, i64] * 4 + [vp, vp, i32, C.c_double, i32, vp, vp, i32, i32]
+                                         + [i64] * 3 + [vp, i32, i32, i64, vp])
+        L.t5_paged_attention_workspace_bytes.argtypes = [i32] * 5 + [C.POINTER(i64)]
+        L.t5_paged_attention.argtypes = ([i32] * 6 + [f32, vp, i64, vp, vp, i32, i32] + [i64] * 3
+                                         + [vp, i32, i64, vp, vp, i32, vp, i64, vp, vp, i64, vp])
+        L.t5_verify_draft.argtypes = ([i32] * 4 + [vp, i64, i64] * 2 + [vp, i64, vp, vp, i64, vp, vp, i64, vp, vp])
         for n in EXPORTS:
             if n != "t5_last_error":
                 getattr(L, n).restype = C.c_int
@@ -371,3 +378,141 @@ def t5_selftest_bounded_wait(status, limit_cycles):
     """One CTA waits, with the kernels' own bounded wait, on a barrier nothing arrives at; it gives up after
     limit_cycles and leaves code 99 in `status` (device int32)."""
     _check(lib().t5_selftest_bounded_wait(_ptr(status), int(limit_cycles), _stream()))
+
+
+# ---- serving.  A call here takes some microseconds on the GPU, so pointers and sizes go to ctypes as plain ints; what a
+# wrong tensor would turn into an access out of range (type, shape, place) is checked first.
+
+def _require(ok, what):
+    if not ok:
+        raise T5Error(-8, what)
+
+
+def _dense(t, name, shape, dtype, device):
+    """A tensor of this shape, type and place whose last dimension is contiguous."""
+    if (t.dtype != dtype or t.device != device or t.shape != shape
+            or (shape[-1] > 1 and t.stride(-1) != 1)):
+        raise T5Error(-8, f"{name}: want a {dtype} tensor {shape} on {device} with a contiguous last dimension, "
+                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _heads(t, name, shape, dtype, device):
+    """[rows, heads, d_kv] whose rows are dense (a column slice of a wider matrix is fine); returns the row stride."""
+    _dense(t, name, shape, dtype, device)
+    _require(shape[1] == 1 or t.stride(1) == shape[2], f"{name}: heads must be adjacent columns")
+    return t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _place(t):
+    """(device, stream) of a call on this tensor; the device has to be the current one."""
+    _require(t.is_cuda and t.device.index == torch.cuda.current_device(), "tensors must lie on the current CUDA device")
+    return t.device, torch.cuda.current_stream().cuda_stream
+
+
+def _dtype_code(t):
+    if t.dtype == torch.bfloat16:
+        return 1
+    _require(t.dtype == torch.float32, "want float32 or bfloat16")
+    return 0
+
+
+def _pool(k_pages, v_pages, table, device):
+    """Arguments that describe the page pools [n_pages, page_size, kv heads, d_kv] (any strides) and the page table."""
+    _require(k_pages.dim() == 4 and table.dim() == 2, "k_pages: want [n_pages, page_size, kv_heads, d_kv]; table: 2-D")
+    shape = tuple(k_pages.shape)
+    _dense(k_pages, "k_pages", shape, k_pages.dtype, device)
+    _dense(v_pages, "v_pages", shape, k_pages.dtype, device)
+    _dense(table, "page_table", tuple(table.shape), torch.int32, device)
+    n, ps, g, d = shape
+    st = [k_pages.stride(i) if shape[i] > 1 else ps * g * d for i in range(3)]      # a single entry has no stride
+    _require(all(v_pages.stride(i) == st[i] or shape[i] == 1 for i in range(3)), "k_pages and v_pages: same strides")
+    ld = table.stride(0) if table.shape[0] > 1 else table.shape[1]
+    return (k_pages.data_ptr(), v_pages.data_ptr(), n, ps, *st, table.data_ptr()), table.shape[1], ld
+
+
+def t5_paged_kv_append(k, v, k_pages, v_pages, page_table, seq_of_token, positions, q=None, q_out=None, rot_dim=0,
+                       rot_base=10000.0, rot_interleaved=False):
+    """k, v [tokens, kv_heads, d_kv] (and q [tokens, heads, d_kv] into q_out) enter the pools; see the header."""
+    device, stream = _place(k)
+    code = _dtype_code(k)
+    _require(k.dim() == 3 and k_pages.dim() == 4 and k_pages.dtype == k.dtype, "k: want [tokens, kv_heads, d_kv] of the pools' type")
+    n, g, d = k.shape
+    _require(tuple(k_pages.shape[2:]) == (g, d), "k_pages: heads or d_kv differ from k")
+    pool, max_pages, ld_table = _pool(k_pages, v_pages, page_table, device)
+    ldk, ldv = _heads(k, "k", (n, g, d), k.dtype, device), _heads(v, "v", (n, g, d), k.dtype, device)
+    _dense(seq_of_token, "seq_of_token", (n,), torch.int32, device)
+    _dense(positions, "positions", (n,), torch.int32, device)
+    h = ldq = ldqo = qp = qop = 0
+    if q is not None:
+        _require(q.dim() == 3 and q_out is not None, "q: want [tokens, heads, d_kv] and q_out")
+        h = q.shape[1]
+        ldq, ldqo = _heads(q, "q", (n, h, d), k.dtype, device), _heads(q_out, "q_out", (n, h, d), k.dtype, device)
+        qp, qop = q.data_ptr(), q_out.data_ptr()
+    _check(lib().t5_paged_kv_append(code, n, h, g, d, qp, ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, qop, ldqo,
+                                    seq_of_token.data_ptr(), positions.data_ptr(), rot_dim, rot_base,
+                                    int(rot_interleaved), *pool, page_table.shape[0], max_pages, ld_table, stream))
+
+
+def t5_paged_attention_workspace_bytes(n_rows, n_q, n_heads, n_kv_heads, d_kv):
+    n = C.c_int64()
+    _check(lib().t5_paged_attention_workspace_bytes(n_rows, n_q, n_heads, n_kv_heads, d_kv, C.byref(n)))
+    return n.value
+
+
+def t5_paged_attention(q, k_pages, v_pages, page_table, lens, out, workspace, scale=1.0, n_q=1, bias=None, lse=None):
+    """q, out [rows, heads, d_kv]; lens [rows]; n_q rows per row of the page table; bias [heads, n_bias] float32, the
+    near end last; lse [rows, heads] float32; see the header."""
+    device, stream = _place(q)
+    code = _dtype_code(q)
+    _require(q.dim() == 3 and k_pages.dim() == 4 and k_pages.dtype == q.dtype, "q: want [rows, heads, d_kv] of the pools' type")
+    r, h, d = q.shape
+    g = k_pages.shape[2]
+    _require(k_pages.shape[3] == d and n_q >= 1 and page_table.dim() == 2 and page_table.shape[0] * n_q == r,
+             "want the pools' d_kv and n_q rows of q per row of the page table")
+    pool, max_pages, ld_table = _pool(k_pages, v_pages, page_table, device)
+    ldq, ldo = _heads(q, "q", (r, h, d), q.dtype, device), _heads(out, "out", (r, h, d), q.dtype, device)
+    _dense(lens, "lens", (r,), torch.int32, device)
+    n_bias = bp = lp = 0
+    if bias is not None:
+        n_bias = bias.shape[-1]
+        _dense(bias, "bias", (h, n_bias), torch.float32, device)
+        _require(bias.is_contiguous(), "bias: want a contiguous tensor")
+        bp = bias.data_ptr()
+    if lse is not None:
+        _dense(lse, "lse", (r, h), torch.float32, device)
+        _require(lse.is_contiguous(), "lse: want a contiguous tensor")
+        lp = lse.data_ptr()
+    _require(workspace.device == device and workspace.is_contiguous(), "workspace: want a contiguous tensor on the device")
+    _check(lib().t5_paged_attention(code, r, n_q, h, g, d, scale, q.data_ptr(), ldq, *pool, max_pages, ld_table,
+                                    lens.data_ptr(), bp, n_bias, out.data_ptr(), ldo, lp, workspace.data_ptr(),
+                                    workspace.numel() * workspace.element_size(), stream))
+
+
+def t5_verify_draft(target, draft, draft_tokens, n_draft, u_accept, u_sample, out_tokens, n_accepted):
+    """target [seqs, drafts + 1, vocab], draft [seqs, drafts, vocab] or None, draft_tokens / u_accept [seqs, drafts],
+    n_draft [seqs] or None, u_sample [seqs] -> out_tokens [seqs, drafts + 1], n_accepted [seqs]; see the header."""
+    device, stream = _place(target)
+    code = _dtype_code(target)
+    _require(target.dim() == 3 and target.shape[1] >= 1, "target: want [seqs, drafts + 1, vocab]")
+    s, k1, v = target.shape
+    k = k1 - 1
+
+    def strides(t, name, shape):
+        _dense(t, name, shape, target.dtype, device)
+        return (t.data_ptr(), t.stride(0) if shape[0] > 1 else 0, t.stride(1) if shape[1] > 1 else v)
+
+    def rows(t, name, dtype, width):
+        _dense(t, name, (s, width), dtype, device)
+        return t.data_ptr(), t.stride(0) if s > 1 else width
+    tgt = strides(target, "target", (s, k1, v))
+    drf = (0, 0, v) if draft is None or k == 0 else strides(draft, "draft", (s, k, v))
+    xs, us = rows(draft_tokens, "draft_tokens", torch.int32, k), rows(u_accept, "u_accept", torch.float32, k)
+    out = rows(out_tokens, "out_tokens", torch.int32, k1)
+    for t, name, dt in ((u_sample, "u_sample", torch.float32), (n_accepted, "n_accepted", torch.int32)):
+        _dense(t, name, (s,), dt, device)
+    np_ = 0
+    if n_draft is not None:
+        _dense(n_draft, "n_draft", (s,), torch.int32, device)
+        np_ = n_draft.data_ptr()
+    _check(lib().t5_verify_draft(code, s, k, v, *tgt, *drf, *xs, np_, *us, u_sample.data_ptr(), *out,
+                                 n_accepted.data_ptr(), stream))
