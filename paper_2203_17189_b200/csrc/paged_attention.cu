@@ -20,6 +20,8 @@
 
 #include <math.h>
 
+#include <atomic>
+
 namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
@@ -161,138 +163,201 @@ __device__ __forceinline__ int64_t key_offset(const AttnParams& a, const Place& 
          (p.k / a.tiles) * a.pool.head_stride;
 }
 
-template <typename T> __device__ __forceinline__ void chunk_floats(const uint4& u, float* f);
-template <> __device__ __forceinline__ void chunk_floats<float>(const uint4& u, float* f) {
-  f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
-}
-template <> __device__ __forceinline__ void chunk_floats<bf16>(const uint4& u, float* f) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-
-// ------------------------------------------------------------------ plain arithmetic (float32 mode)
-// Warp tile of KT keys: lane = (key, part of the columns) for the scores, lane = columns for the values.
-template <typename T, int DK, int RT> struct Simt {
-  static constexpr int ES = sizeof(T), CPR = DK * ES / 16, N = 16 / ES;
-  static constexpr int KT = 4096 / (DK * ES) < 32 ? 4096 / (DK * ES) : 32;
+// Shape of a warp's tiles: KT keys of DK columns of ES bytes, K then V, in a ring of STAGES.  4 KB of each where 32 lanes
+// can name the keys.  Measured with 2, 3 and 4 stages: three are within 1 % of four and leave room for a second CTA.
+template <int ES, int DK> struct Tile {
+  static constexpr int ROW = DK * ES, CPR = ROW / 16;
+  static constexpr int KT = 4096 / ROW < 32 ? 4096 / ROW : 32;
   static constexpr int BK = KT * kWarps;
-  static constexpr int TILE = KT * DK * ES, STAGES = 3;
-  static constexpr int PARTS = 32 / KT, CL = CPR / PARTS;      // lanes per key, chunks per lane
-  static constexpr int VC = DK / 32;                           // output columns per lane
-  static constexpr int QS = RT * DK * 4;                       // float32 query rows of a warp
-  static constexpr int SMEM = kWarps * (STAGES * 2 * TILE + QS + STAGES * 4) + kWarps * RT * (DK + 2) * 4;
+  static constexpr int BYTES = KT * ROW, STAGES = 3;
+  static constexpr int RING = STAGES * 2 * BYTES;
 };
 
-template <typename T, int DK, int RT>
-__global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_constant__ AttnParams a) {
-  pdl_sync();
-  using L = Simt<T, DK, RT>;
-  extern __shared__ __align__(128) unsigned char smem[];
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-  unsigned char* ring = smem + w * (L::STAGES * 2 * L::TILE);
-  float* qs = reinterpret_cast<float*>(smem + kWarps * (L::STAGES * 2 * L::TILE) + w * L::QS);
-  uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * (L::STAGES * 2 * L::TILE + L::QS)) + w * L::STAGES;
-  float* merge = reinterpret_cast<float*>(smem + kWarps * (L::STAGES * 2 * L::TILE + L::QS + L::STAGES * 4));
-  const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
+// A warp's stream of tiles: runs ahead of the arithmetic by STAGES - 1 tiles, over the ends of items.
+template <typename L> struct KeyStream {
+  const AttnParams& a;
+  Place at;             // of the next tile to be copied
+  int64_t left;         // tiles still to be copied
+  int64_t off;          // this lane's key of that tile: its page has been looked up one step ahead
+  unsigned char* ring;
+  uint32_t ring_s;
+  uint32_t* vmask;      // per stage: which keys of the tile exist
+  int w, lane;
 
-  int64_t x0, x1;
-  Place cur;
-  find_share(a, L::BK, x0, x1, cur);
-  if (x0 == x1) {
-    if (tid == 0) a.meta[blockIdx.x] = make_int4(-1, 0, -1, 0);
-    return;
+  __device__ __forceinline__ void lookup() {
+    off = left > 0 && lane < L::KT ? key_offset(a, at, at.blk * L::BK + w * L::KT + lane) : -1;
   }
-  int4 meta = make_int4(-1, 0, -1, 0);
-  Place nxt = cur;                   // runs ahead of cur by the stages in flight
-  int64_t to_issue = x1 - x0;
-
-  auto lookup = [&]() -> int64_t {
-    if (to_issue <= 0 || lane >= L::KT) return -1;
-    return key_offset(a, nxt, nxt.blk * L::BK + w * L::KT + lane);
-  };
-  auto issue = [&](int stage, int64_t off) {
-    if (to_issue > 0) {
+  __device__ __forceinline__ void issue(int stage) {
+    if (left > 0) {
       const uint32_t ok = __ballot_sync(0xffffffffu, off >= 0);
       if (lane == 0) vmask[stage] = ok;
-      const uint32_t kd = ring_s + stage * 2 * L::TILE, vd = kd + L::TILE;
+      const uint32_t kd = ring_s + stage * 2 * L::BYTES, vd = kd + L::BYTES;
       const int c = lane % L::CPR;
 #pragma unroll
       for (int i = 0; i < L::KT * L::CPR / 32; ++i) {
         const int row = lane / L::CPR + i * (32 / L::CPR);
         const int64_t o = __shfl_sync(0xffffffffu, off, row);
-        const uint32_t d = row * (DK * L::ES) + swz<L::CPR>(row, c) * 16;
+        const uint32_t d = row * L::ROW + swz<L::CPR>(row, c) * 16;
         const int64_t src = o >= 0 ? o + c * 16 : 0;
-        cp_async16(kd + d, a.pool.k + src, o >= 0);
+        cp_async16(kd + d, a.pool.k + src, o >= 0);      // a key that does not exist becomes zeros
         cp_async16(vd + d, a.pool.v + src, o >= 0);
       }
-      step(a, L::BK, nxt);
-      --to_issue;
+      step(a, L::BK, at);
+      --left;
     }
     cp_async_commit();
-  };
-
-  int64_t off = lookup();
+    lookup();
+  }
+  __device__ __forceinline__ KeyStream(const AttnParams& p, const Place& from, int64_t n, unsigned char* r, uint32_t* vm,
+                                       int warp, int ln)
+      : a(p), at(from), left(n), ring(r), ring_s((uint32_t)__cvta_generic_to_shared(r)), vmask(vm), w(warp), lane(ln) {
+    lookup();
 #pragma unroll
-  for (int i = 0; i < L::STAGES - 1; ++i) { issue(i, off); off = lookup(); }
+    for (int i = 0; i < L::STAGES - 1; ++i) issue(i);
+  }
+};
+
+// The query rows of an item and what is known of them
+struct Rows {
+  int r0, n, g;      // first row of the tile, rows in it, kv head
+  __device__ __forceinline__ Rows(const AttnParams& a, const Place& p, int rt)
+      : r0((p.k % a.tiles) * rt), n(min(rt, a.n_q * a.m - (p.k % a.tiles) * rt)), g(p.k / a.tiles) {}
+  __device__ __forceinline__ int token(const AttnParams& a, const Place& p, int r) const { return p.s * a.n_q + (r0 + r) / a.m; }
+  __device__ __forceinline__ int head(const AttnParams& a, int r) const { return g * a.m + (r0 + r) % a.m; }
+};
+
+// End of an item or of the share: joins the warps' rows [from, from + MR) (merge [warp][MR][DK + 2]: output, maximum, sum;
+// written by the caller) and writes the finished rows, or the piece.  Called by all threads.  A few rows at a time keep
+// the buffer small enough for two CTAs per SM.
+template <typename T, int DK, int RT, int MR>
+__device__ __forceinline__ void finish_rows(const AttnParams& a, const Place& p, const float* merge, bool whole, int slot,
+                                            int from) {
+  __syncthreads();
+  const Rows rows(a, p, RT);
+  for (int idx = threadIdx.x; idx < min(rows.n - from, MR) * DK; idx += kThreads) {
+    const int mr = idx / DK, c = idx % DK, r = from + mr;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) mx = fmaxf(mx, merge[(i * MR + mr) * (DK + 2) + DK]);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float acc = 0.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const float* mg = merge + (i * MR + mr) * (DK + 2);
+      const float f = exp2f((mg[DK] - ref) * kLog2e);
+      acc += f * mg[c];
+      sum += f * mg[DK + 1];
+    }
+    if (whole) {
+      const int h = rows.head(a, r), row = rows.token(a, p, r);
+      reinterpret_cast<T*>(a.out + (int64_t)row * a.ldo)[h * DK + c] = from_f<T>(sum == 0.f ? 0.f : acc / sum);
+      if (c == 0 && a.lse != nullptr) a.lse[(int64_t)row * a.H + h] = sum == 0.f ? -INFINITY : mx + logf(sum);
+    } else {
+      float* pt = a.part + (((int64_t)blockIdx.x * 2 + slot) * a.rows + r) * (DK + 2);
+      pt[c] = acc;
+      if (c == 0) { pt[DK] = mx; pt[DK + 1] = sum; }
+    }
+  }
+  __syncthreads();
+}
+
+// Bookkeeping of a CTA's walk over its share: which piece an item's end leaves where (see AttnParams::meta)
+struct Pieces {
+  int4 meta = make_int4(-1, 0, -1, 0);
+  bool starts_here;
+  __device__ __forceinline__ bool whole(bool item_ends) const { return item_ends && starts_here; }
+  __device__ __forceinline__ int slot() const { return starts_here ? 1 : 0; }
+  __device__ __forceinline__ void note(const AttnParams& a, const Place& p, bool item_ends) {
+    const int item = p.s * (a.G * a.tiles) + p.k;
+    if (!whole(item_ends)) {
+      if (starts_here) meta.z = item;
+      else { meta.x = item; meta.y = item_ends ? 0 : 1; }
+    }
+    starts_here = true;
+  }
+};
+
+__device__ __forceinline__ void report_length(const AttnParams& a, int row) {
+  if (a.lens[row] > a.cap) paged_report(a.status, PAGED_BAD_LENGTH);
+}
+
+// ------------------------------------------------------------------ float32: plain arithmetic
+// Lane = (key, part of the columns) for the scores, lane = columns for the values.
+template <int DK, int RT> struct Simt : Tile<4, DK> {
+  using B = Tile<4, DK>;
+  static constexpr int PARTS = 32 / B::KT, CL = B::CPR / PARTS;      // lanes per key, chunks per lane
+  static constexpr int VC = DK / 32;                                 // output columns per lane
+  static constexpr int QS = RT * DK * 4;                             // query rows of the item
+  static constexpr int MR = RT < 4 ? RT : 4;
+  static constexpr int SMEM = kWarps * (B::RING + B::STAGES * 4) + QS + kWarps * MR * (DK + 2) * 4;
+};
+
+template <int DK, int RT>
+__global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_constant__ AttnParams a) {
+  pdl_sync();
+  using L = Simt<DK, RT>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  float* qs = reinterpret_cast<float*>(smem + kWarps * L::RING);
+  uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * L::RING + L::QS) + w * L::STAGES;
+  float* merge = reinterpret_cast<float*>(smem + kWarps * (L::RING + L::STAGES * 4) + L::QS);
+
+  int64_t x0, x1;
+  Place cur;
+  find_share(a, L::BK, x0, x1, cur);
+  Pieces pieces;
+  if (x0 == x1) {
+    if (tid == 0) a.meta[blockIdx.x] = pieces.meta;
+    return;
+  }
+  pieces.starts_here = cur.blk == 0;
+  KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, w, lane);
 
   const int key_l = lane % L::KT, part_l = lane / L::KT;
   float m[RT], l[RT], o[RT][L::VC];
   int len[RT];
-  bool starts_here = cur.blk == 0;
   bool fresh = true;
   int stage = 0;
   for (int64_t x = x0; x < x1; ++x) {
-    const int r0 = (cur.k % a.tiles) * RT, nr = min(RT, a.n_q * a.m - r0);      // query rows of the item
-    const int g = cur.k / a.tiles;
+    const Rows rows(a, cur, RT);
+    const int nr = rows.n;
     if (fresh) {
       fresh = false;
-      __syncwarp();
-      for (int idx = lane; idx < RT * DK; idx += 32) {
-        const int r = r0 + idx / DK;
-        float v = 0.f;
-        if (idx / DK < nr)
-          v = to_f(reinterpret_cast<const T*>(a.q + (int64_t)(cur.s * a.n_q + r / a.m) * a.ldq)[(g * a.m + r % a.m) * DK + idx % DK]);
-        qs[idx] = v;
+      for (int idx = tid; idx < RT * DK; idx += kThreads) {
+        const int r = idx / DK;
+        qs[idx] = r < nr ? reinterpret_cast<const float*>(a.q + (int64_t)rows.token(a, cur, r) * a.ldq)[rows.head(a, r) * DK + idx % DK] : 0.f;
       }
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         m[r] = -INFINITY; l[r] = 0.f;
-        len[r] = r < nr ? row_len(a, cur.s * a.n_q + (r0 + r) / a.m) : 0;
+        len[r] = r < nr ? row_len(a, rows.token(a, cur, r)) : 0;
 #pragma unroll
         for (int c = 0; c < L::VC; ++c) o[r][c] = 0.f;
-        if (r < nr && lane == 0 && a.lens[cur.s * a.n_q + (r0 + r) / a.m] > a.cap) paged_report(a.status, PAGED_BAD_LENGTH);
       }
+      if (tid < nr) report_length(a, rows.token(a, cur, tid));
+      __syncthreads();      // the last item's reads of qs lie before the barriers of finish_rows
     }
     cp_async_wait<L::STAGES - 2>();
     __syncwarp();
-    issue((stage + L::STAGES - 1) % L::STAGES, off);
-    off = lookup();
+    keys.issue((stage + L::STAGES - 1) % L::STAGES);
     const int j0 = cur.blk * L::BK + w * L::KT, j = j0 + key_l;
     const uint32_t ok = vmask[stage];
     if (ok != 0) {
-      const unsigned char* kt = ring + stage * 2 * L::TILE;
-      const unsigned char* vt = kt + L::TILE;
+      const unsigned char* kt = keys.ring + stage * 2 * L::BYTES;
+      const unsigned char* vt = kt + L::BYTES;
       float sc[RT];
 #pragma unroll
       for (int r = 0; r < RT; ++r) sc[r] = 0.f;
 #pragma unroll
       for (int c = 0; c < L::CL; ++c) {
         const int ch = part_l * L::CL + c;
-        float kf[L::N];
-        chunk_floats<T>(*reinterpret_cast<const uint4*>(kt + key_l * (DK * L::ES) + swz<L::CPR>(key_l, ch) * 16), kf);
+        const float4 k4 = *reinterpret_cast<const float4*>(kt + key_l * L::ROW + swz<L::CPR>(key_l, ch) * 16);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
           if (r < nr) {
-#pragma unroll
-            for (int i = 0; i < L::N; i += 4) {
-              const float4 q4 = *reinterpret_cast<const float4*>(qs + r * DK + ch * L::N + i);
-              sc[r] = fmaf(q4.x, kf[i], sc[r]); sc[r] = fmaf(q4.y, kf[i + 1], sc[r]);
-              sc[r] = fmaf(q4.z, kf[i + 2], sc[r]); sc[r] = fmaf(q4.w, kf[i + 3], sc[r]);
-            }
+            const float4 q4 = *reinterpret_cast<const float4*>(qs + r * DK + ch * 4);
+            sc[r] = fmaf(q4.x, k4.x, sc[r]); sc[r] = fmaf(q4.y, k4.y, sc[r]);
+            sc[r] = fmaf(q4.z, k4.z, sc[r]); sc[r] = fmaf(q4.w, k4.w, sc[r]);
           }
         }
       }
@@ -303,8 +368,7 @@ __global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_
           for (int of = L::KT; of < 32; of <<= 1) sc[r] += __shfl_xor_sync(0xffffffffu, sc[r], of);
           const bool seen = ((ok >> key_l) & 1) && j < len[r];
           float s = sc[r] * a.scale;
-          if (a.bias != nullptr && seen)
-            s += a.bias[(int64_t)(g * a.m + (r0 + r) % a.m) * a.n_bias + max(a.n_bias - len[r] + j, 0)];
+          if (a.bias != nullptr && seen) s += a.bias[(int64_t)rows.head(a, r) * a.n_bias + max(a.n_bias - len[r] + j, 0)];
           s = seen ? s : -INFINITY;
           float mx = s;
 #pragma unroll
@@ -324,13 +388,9 @@ __global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_
       }
 #pragma unroll 8
       for (int kk = 0; kk < L::KT; ++kk) {
-        float vf[L::VC];
-        const int byte = lane * L::VC * L::ES;
-        const unsigned char* at = vt + kk * (DK * L::ES) + swz<L::CPR>(kk, byte >> 4) * 16 + (byte & 15);
-        struct alignas(L::VC * L::ES) Cols { T v[L::VC]; };
-        const Cols cols = *reinterpret_cast<const Cols*>(at);
-#pragma unroll
-        for (int c = 0; c < L::VC; ++c) vf[c] = to_f(cols.v[c]);
+        struct alignas(L::VC * 4) Cols { float v[L::VC]; };
+        const int byte = lane * L::VC * 4;
+        const Cols vf = *reinterpret_cast<const Cols*>(vt + kk * L::ROW + swz<L::CPR>(kk, byte >> 4) * 16 + (byte & 15));
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
           if (r < nr) {
@@ -338,66 +398,297 @@ __global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_
             // a key this row does not see has weight 0 and may hold anything: its value must not enter
             const bool seen = RT == 1 || j0 + kk < len[r];
 #pragma unroll
-            for (int c = 0; c < L::VC; ++c) o[r][c] = seen ? fmaf(p, vf[c], o[r][c]) : o[r][c];
+            for (int c = 0; c < L::VC; ++c) o[r][c] = seen ? fmaf(p, vf.v[c], o[r][c]) : o[r][c];
           }
         }
       }
     }
     stage = (stage + 1) % L::STAGES;
-    // end of the item or of the share: join the warps, write the rows or the piece
     const bool item_ends = cur.blk + 1 == cur.nb;
     if (item_ends || x + 1 == x1) {
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        if (r < nr) {
-          float lt = part_l == 0 ? l[r] : 0.f;
+      for (int from = 0; from < RT; from += L::MR) {
+        if (from < nr) {
 #pragma unroll
-          for (int of = 16; of > 0; of >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
-          float* mg = merge + (w * RT + r) * (DK + 2);
+          for (int mr = 0; mr < L::MR; ++mr) {
+            const int r = from + mr;
+            float lt = part_l == 0 ? l[r] : 0.f;
 #pragma unroll
-          for (int c = 0; c < L::VC; ++c) mg[lane * L::VC + c] = o[r][c];
-          if (lane == 0) { mg[DK] = m[r]; mg[DK + 1] = lt; }
+            for (int of = 16; of > 0; of >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
+            float* mg = merge + (w * L::MR + mr) * (DK + 2);
+#pragma unroll
+            for (int c = 0; c < L::VC; ++c) mg[lane * L::VC + c] = o[r][c];
+            if (lane == 0) { mg[DK] = m[r]; mg[DK + 1] = lt; }
+          }
+          finish_rows<float, DK, RT, L::MR>(a, cur, merge, pieces.whole(item_ends), pieces.slot(), from);
         }
       }
-      __syncthreads();
-      const bool whole = item_ends && starts_here;
-      const int item = cur.s * (a.G * a.tiles) + cur.k;
-      const int slot = starts_here ? 1 : 0;
-      if (!whole) {
-        if (slot == 0) { meta.x = item; meta.y = item_ends ? 0 : 1; } else meta.z = item;
-      }
-      for (int idx = tid; idx < nr * DK; idx += kThreads) {
-        const int r = idx / DK, c = idx % DK;
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kWarps; ++i) mx = fmaxf(mx, merge[(i * RT + r) * (DK + 2) + DK]);
-        const float ref = mx == -INFINITY ? 0.f : mx;
-        float acc = 0.f, sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < kWarps; ++i) {
-          const float* mg = merge + (i * RT + r) * (DK + 2);
-          const float f = exp2f((mg[DK] - ref) * kLog2e);
-          acc += f * mg[c];
-          sum += f * mg[DK + 1];
-        }
-        if (whole) {
-          const int rr = r0 + r, h = g * a.m + rr % a.m, row = cur.s * a.n_q + rr / a.m;
-          reinterpret_cast<T*>(a.out + (int64_t)row * a.ldo)[h * DK + c] = from_f<T>(sum == 0.f ? 0.f : acc / sum);
-          if (c == 0 && a.lse != nullptr) a.lse[(int64_t)row * a.H + h] = sum == 0.f ? -INFINITY : mx + logf(sum);
-        } else {
-          float* pt = a.part + (((int64_t)blockIdx.x * 2 + slot) * a.rows + r) * (DK + 2);
-          pt[c] = acc;
-          if (c == 0) { pt[DK] = mx; pt[DK + 1] = sum; }
-        }
-      }
-      __syncthreads();
+      pieces.note(a, cur, item_ends);
       fresh = true;
-      starts_here = true;
     }
     step(a, L::BK, cur);
   }
   cp_async_wait<0>();
-  if (tid == 0) a.meta[blockIdx.x] = meta;
+  if (tid == 0) a.meta[blockIdx.x] = pieces.meta;
+}
+
+// ------------------------------------------------------------------ bfloat16: matrix instructions
+// S = Q K^T and O += P V as m16n8k16 products (float32 sums) whose 16 rows are query rows: heads that share the kv head,
+// and the new tokens of the sequence.  A single row fills a sixteenth of them, and the tensor pipe is idle all the same:
+// what counts is that a key costs few instructions.  tcgen05 needs 64 or 128 rows and a trip through tensor memory per
+// tile; here neither operand nor result leaves the registers between load and use.
+// RT = 8 leaves the lower half of the rows out of the softmax and of the registers.
+// The weights go into the second product as a sum of two bfloat16 parts (error 2^-17 instead of 2^-9 for 8 more matrix
+// instructions per 16 keys, on a pipe that has the room), so the output is the float32 result rounded once.
+template <int DK, int RT> struct Mma : Tile<2, DK> {
+  using B = Tile<2, DK>;
+  static constexpr int SMEM = kWarps * (B::RING + B::STAGES * 4) + kWarps * 8 * (DK + 2) * 4;
+};
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// c[0..1]: rows lane / 4, c[2..3]: rows lane / 4 + 8 (H16; otherwise those rows are zero and not kept)
+template <bool H16>
+__device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (H16) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  } else {
+    float z0, z1;
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%5}, {%7,%8}, {%0,%1,%9,%9};"
+                 : "+f"(c[0]), "+f"(c[1]), "=f"(z0), "=f"(z1) : "r"(a0), "r"(0), "r"(a2), "r"(b0), "r"(b1), "f"(0.f));
+  }
+}
+// two floats as bfloat16 parts: hi = round(x), lo = round(x - hi)
+__device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  hi = *reinterpret_cast<const uint32_t*>(&h);
+  const float2 f = __bfloat1622float2(h);
+  const __nv_bfloat162 l = __floats2bfloat162_rn(x - f.x, y - f.y);
+  lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+
+template <int DK, int RT>
+__global__ void __launch_bounds__(kThreads) paged_attn_mma_kernel(const __grid_constant__ AttnParams a) {
+  pdl_sync();
+  using L = Mma<DK, RT>;
+  constexpr bool H16 = RT == 16;
+  constexpr int NH = RT / 8;             // row halves: this lane's rows are lane / 4 (+ 8)
+  constexpr int KS = DK / 16, NG = L::KT / 16, NT = DK / 8, CN = 2 * NH;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, quad = lane & 3;
+  uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * L::RING) + w * L::STAGES;
+  float* merge = reinterpret_cast<float*>(smem + kWarps * (L::RING + L::STAGES * 4));
+
+  int64_t x0, x1;
+  Place cur;
+  find_share(a, L::BK, x0, x1, cur);
+  Pieces pieces;
+  if (x0 == x1) {
+    if (tid == 0) a.meta[blockIdx.x] = pieces.meta;
+    return;
+  }
+  pieces.starts_here = cur.blk == 0;
+  KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, w, lane);
+
+  uint32_t qf[KS][2 * NH];               // A operand: columns 16 ks + 2 quad (+ 8), rows lane / 4 (+ 8)
+  float m[NH], l[NH], o[NT][CN], far[NH];
+  const float* bias[NH];
+  int len[NH], min_len = 0;
+  bool fresh = true;
+  int stage = 0;
+  for (int64_t x = x0; x < x1; ++x) {
+    if (fresh) {
+      fresh = false;
+      const Rows rows(a, cur, RT);
+      min_len = 0x7fffffff;
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf) {
+        const int r = lane / 4 + 8 * hf;
+        const bool valid = r < rows.n;
+        m[hf] = -INFINITY; l[hf] = 0.f; len[hf] = 0; far[hf] = 0.f; bias[hf] = nullptr;
+        const uint32_t* src = nullptr;
+        if (valid) {
+          const int row = rows.token(a, cur, r), h = rows.head(a, r);
+          len[hf] = row_len(a, row);
+          min_len = min(min_len, len[hf]);
+          src = reinterpret_cast<const uint32_t*>(a.q + (int64_t)row * a.ldq + h * (DK * 2)) + quad;
+          if (a.bias != nullptr) { bias[hf] = a.bias + (int64_t)h * a.n_bias; far[hf] = bias[hf][0]; }
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          qf[ks][hf] = valid ? src[ks * 8] : 0u;
+          qf[ks][NH + hf] = valid ? src[ks * 8 + 4] : 0u;
+        }
+      }
+#pragma unroll
+      for (int of = 4; of < 32; of <<= 1) min_len = min(min_len, __shfl_xor_sync(0xffffffffu, min_len, of));
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < CN; ++i) o[t][i] = 0.f;
+      if (tid < rows.n) report_length(a, rows.token(a, cur, tid));
+    }
+    cp_async_wait<L::STAGES - 2>();
+    __syncwarp();
+    keys.issue((stage + L::STAGES - 1) % L::STAGES);
+    const int j0 = cur.blk * L::BK + w * L::KT;
+    const uint32_t ok = vmask[stage];
+    if (ok != 0) {
+      const uint32_t kt = keys.ring_s + stage * 2 * L::BYTES, vt = kt + L::BYTES;
+      float s[NG * 2][CN];
+#pragma unroll
+      for (int t = 0; t < NG * 2; ++t)
+#pragma unroll
+        for (int i = 0; i < CN; ++i) s[t][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          uint32_t b[4];
+          const int row = g * 16 + (lane & 7) + ((lane >> 4) & 1) * 8;
+          ldsm4(kt + row * L::ROW + swz<L::CPR>(row, 2 * ks + ((lane >> 3) & 1)) * 16, b);
+          mma16816<H16>(s[2 * g], qf[ks][0], qf[ks][NH - 1], qf[ks][NH], qf[ks][2 * NH - 1], b[0], b[1]);
+          mma16816<H16>(s[2 * g + 1], qf[ks][0], qf[ks][NH - 1], qf[ks][NH], qf[ks][2 * NH - 1], b[2], b[3]);
+        }
+      }
+      // scores: scale, bias, mask.  Behind the distance where the bias saturates it is one value per row.
+      const bool near = a.bias != nullptr && a.n_bias - min_len + j0 + L::KT - 1 > 0;
+      const bool all_seen = ok == (L::KT == 32 ? 0xffffffffu : (1u << L::KT) - 1u) && j0 + L::KT <= min_len;
+      float top[NH];
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf) top[hf] = m[hf];
+#pragma unroll
+      for (int t = 0; t < NG * 2; ++t)
+#pragma unroll
+        for (int i = 0; i < CN; ++i) {
+          const int hf = i >> 1, kk = t * 8 + quad * 2 + (i & 1);
+          float v = s[t][i] * a.scale;
+          if (near) {
+            if (bias[hf] != nullptr && j0 + kk < len[hf]) v += bias[hf][max(a.n_bias - len[hf] + j0 + kk, 0)];
+          } else {
+            v += far[hf];
+          }
+          if (!all_seen && !(((ok >> kk) & 1) && j0 + kk < len[hf])) v = -INFINITY;
+          s[t][i] = v;
+          top[hf] = fmaxf(top[hf], v);
+        }
+      float ref[NH];
+      bool moved = false;
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf) {
+        top[hf] = fmaxf(top[hf], __shfl_xor_sync(0xffffffffu, top[hf], 1));
+        top[hf] = fmaxf(top[hf], __shfl_xor_sync(0xffffffffu, top[hf], 2));
+        ref[hf] = top[hf] == -INFINITY ? 0.f : top[hf];
+        moved |= top[hf] != m[hf];
+      }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int hf = 0; hf < NH; ++hf) {
+          const float corr = exp2f((m[hf] - ref[hf]) * kLog2e);
+          l[hf] *= corr;
+          m[hf] = top[hf];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) { o[t][2 * hf] *= corr; o[t][2 * hf + 1] *= corr; }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NG * 2; ++t)
+#pragma unroll
+        for (int i = 0; i < CN; ++i) {
+          const int hf = i >> 1;
+          s[t][i] = exp2f((s[t][i] - ref[hf]) * kLog2e);      // differences first: a bias of the lowest float stays finite
+          l[hf] += s[t][i];
+        }
+      // Keys that one row sees and another does not have weight 0 there, and 0 x NaN would spoil the row: if such a tile
+      // holds a value that is not finite, it is taken key by key.
+      bool plain = false;
+      if (j0 + L::KT > min_len) {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < L::BYTES / 512; ++i) {
+          uint32_t u[4];
+          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                       : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(vt + (i * 32 + lane) * 16) : "memory");
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            bad |= (u[k] & 0x7f80u) == 0x7f80u || (u[k] & 0x7f800000u) == 0x7f800000u;
+        }
+        plain = __any_sync(0xffffffffu, bad);
+      }
+      if (!plain) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          uint32_t hi[4] = {0u, 0u, 0u, 0u}, lo[4] = {0u, 0u, 0u, 0u};
+          split2(s[2 * g][0], s[2 * g][1], hi[0], lo[0]);
+          split2(s[2 * g + 1][0], s[2 * g + 1][1], hi[2], lo[2]);
+          if (H16) {
+            split2(s[2 * g][CN - 2], s[2 * g][CN - 1], hi[1], lo[1]);
+            split2(s[2 * g + 1][CN - 2], s[2 * g + 1][CN - 1], hi[3], lo[3]);
+          }
+#pragma unroll
+          for (int t = 0; t < NT; t += 2) {
+            uint32_t b[4];
+            const int row = g * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
+            ldsm4_t(vt + row * L::ROW + swz<L::CPR>(row, t + ((lane >> 4) & 1)) * 16, b);
+            mma16816<H16>(o[t], hi[0], hi[1], hi[2], hi[3], b[0], b[1]);
+            mma16816<H16>(o[t + 1], hi[0], hi[1], hi[2], hi[3], b[2], b[3]);
+            mma16816<H16>(o[t], lo[0], lo[1], lo[2], lo[3], b[0], b[1]);
+            mma16816<H16>(o[t + 1], lo[0], lo[1], lo[2], lo[3], b[2], b[3]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < L::KT; ++kk) {
+#pragma unroll
+          for (int hf = 0; hf < NH; ++hf) {
+            const float p = __shfl_sync(0xffffffffu, s[kk / 8][2 * hf + (kk & 1)], (lane & ~3) | ((kk & 7) >> 1));
+            if (j0 + kk < len[hf]) {
+#pragma unroll 1
+              for (int t = 0; t < NT; ++t) {
+                uint32_t u;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u) : "r"(vt + kk * L::ROW + swz<L::CPR>(kk, t) * 16 + quad * 4) : "memory");
+                const float v0 = __uint_as_float(u << 16), v1 = __uint_as_float(u & 0xffff0000u);
+#pragma unroll
+                for (int tt = 0; tt < NT; ++tt)      // o is indexed by constants only: it stays in registers
+                  if (tt == t) { o[tt][2 * hf] = fmaf(p, v0, o[tt][2 * hf]); o[tt][2 * hf + 1] = fmaf(p, v1, o[tt][2 * hf + 1]); }
+              }
+            }
+          }
+        }
+      }
+    }
+    stage = (stage + 1) % L::STAGES;
+    const bool item_ends = cur.blk + 1 == cur.nb;
+    if (item_ends || x + 1 == x1) {
+      const int n = Rows(a, cur, RT).n;
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf) {
+        float lt = l[hf];
+        lt += __shfl_xor_sync(0xffffffffu, lt, 1);
+        lt += __shfl_xor_sync(0xffffffffu, lt, 2);
+        if (8 * hf + lane / 4 < n) {
+          float* mg = merge + (w * 8 + lane / 4) * (DK + 2);
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            *reinterpret_cast<float2*>(mg + t * 8 + quad * 2) = make_float2(o[t][2 * hf], o[t][2 * hf + 1]);
+          if (quad == 0) { mg[DK] = m[hf]; mg[DK + 1] = lt; }
+        }
+        if (8 * hf < n) finish_rows<bf16, DK, RT, 8>(a, cur, merge, pieces.whole(item_ends), pieces.slot(), 8 * hf);
+      }
+      pieces.note(a, cur, item_ends);
+      fresh = true;
+    }
+    step(a, L::BK, cur);
+  }
+  cp_async_wait<0>();
+  if (tid == 0) a.meta[blockIdx.x] = pieces.meta;
 }
 
 // Joins the pieces of the item that the boundary behind CTA blockIdx.x cuts first; one CTA per boundary and query row.
@@ -463,43 +754,51 @@ __global__ void __launch_bounds__(128) paged_attn_join_kernel(const __grid_const
   }
 }
 
-int sm_count() {
-  static int cached[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-  if (cached[dev] == 0) {
-    int n = 0;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 148;
-    cached[dev] = n;
-  }
-  return cached[dev];
-}
+using Kernel = void (*)(AttnParams);
 
-// Rows of one tile
-int row_tile(int rows) { return rows == 1 ? 1 : 8; }
-
+// CTAs that fill the GPU with this kernel, looked up once per device
 template <typename T, int DK, int RT>
-cudaError_t run_simt(AttnParams& a, cudaStream_t st) {
-  using L = Simt<T, DK, RT>;
-  static bool set[64];
+cudaError_t grid_of(Kernel kernel, int smem, int* ctas) {
+  static std::atomic<int> known[64];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  if (!set[dev]) {
-    e = cudaFuncSetAttribute(paged_attn_simt_kernel<T, DK, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM);
+  int n = known[dev].load(std::memory_order_acquire);
+  if (n == 0) {
+    int sms = 0, per_sm = 0;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, smem);
     if (e != cudaSuccess) return e;
-    set[dev] = true;
+    n = sms * per_sm < kMaxCtas ? sms * per_sm : kMaxCtas;
+    if (n < 2) n = 2;
+    known[dev].store(n, std::memory_order_release);
   }
-  int occ = 227 * 1024 / (L::SMEM + 1024);
-  occ = occ > 3 ? 3 : (occ < 1 ? 1 : occ);
-  int ctas = sm_count() * occ;
-  if (ctas > kMaxCtas) ctas = kMaxCtas;
+  *ctas = n;
+  return cudaSuccess;
+}
+
+template <typename T, int DK, int RT>
+cudaError_t run_attention(AttnParams& a, Kernel kernel, int smem, cudaStream_t st) {
+  int ctas = 0;
+  cudaError_t e = grid_of<T, DK, RT>(kernel, smem, &ctas);
+  if (e != cudaSuccess) return e;
   a.tiles = (a.n_q * a.m + RT - 1) / RT;
   a.rows = a.n_q * a.m < RT ? a.n_q * a.m : RT;
-  e = launch_pdl(paged_attn_simt_kernel<T, DK, RT>, dim3(ctas), dim3(kThreads), (size_t)L::SMEM, st, a);
+  e = launch_pdl(kernel, dim3(ctas), dim3(kThreads), (size_t)smem, st, a);
   if (e != cudaSuccess) return e;
   return launch_pdl(paged_attn_join_kernel<T, DK, RT>, dim3(ctas - 1, a.rows), dim3(128), 0, st, a, ctas);
+}
+// Rows of a tile: one row alone spares the float32 kernel seven eighths of its arithmetic; 8 rows half of the matrix
+// kernel's softmax
+template <int DK> cudaError_t run_f32(AttnParams& a, cudaStream_t st) {
+  if (a.n_q * a.m == 1) return run_attention<float, DK, 1>(a, paged_attn_simt_kernel<DK, 1>, Simt<DK, 1>::SMEM, st);
+  return run_attention<float, DK, 8>(a, paged_attn_simt_kernel<DK, 8>, Simt<DK, 8>::SMEM, st);
+}
+template <int DK> cudaError_t run_bf16(AttnParams& a, cudaStream_t st) {
+  if (a.n_q * a.m <= 8) return run_attention<bf16, DK, 8>(a, paged_attn_mma_kernel<DK, 8>, Mma<DK, 8>::SMEM, st);
+  return run_attention<bf16, DK, 16>(a, paged_attn_mma_kernel<DK, 16>, Mma<DK, 16>::SMEM, st);
 }
 
 }  // namespace
@@ -522,11 +821,8 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& g, cudaStream_t st) {
   a.pool = g.pool; a.status = g.status;
   a.meta = (int4*)g.workspace;
   a.part = (float*)((char*)g.workspace + kMaxCtas * sizeof(int4));
-  const int rt = row_tile(a.n_q * a.m);
-#define RUN(T, DK) (rt == 1 ? run_simt<T, DK, 1>(a, st) : run_simt<T, DK, 8>(a, st))
-  if (g.dtype == DT_F32) return g.d_kv == 32 ? RUN(float, 32) : g.d_kv == 64 ? RUN(float, 64) : RUN(float, 128);
-  return g.d_kv == 32 ? RUN(bf16, 32) : g.d_kv == 64 ? RUN(bf16, 64) : RUN(bf16, 128);
-#undef RUN
+  if (g.dtype == DT_F32) return g.d_kv == 32 ? run_f32<32>(a, st) : g.d_kv == 64 ? run_f32<64>(a, st) : run_f32<128>(a, st);
+  return g.d_kv == 32 ? run_bf16<32>(a, st) : g.d_kv == 64 ? run_bf16<64>(a, st) : run_bf16<128>(a, st);
 }
 
 extern "C" {
