@@ -6,15 +6,17 @@
 // serves query heads g m .. g m + m - 1.
 //
 // Bound: memory (the cache is read once; 4 FLOP per cached value and query row).  So the work is cut by bytes, not by
-// rows: the cache of all sequences and kv heads is one line of blocks (an "item" = one sequence, one kv head, one tile
-// of query rows; a block = kBK keys of an item), and CTA c of a grid that fills the GPU takes the c-th equal share of
-// that line, wherever the lengths put its ends.  A running maximum and sum per query row make one pass over the data
-// enough; an item that ends inside one CTA is written at once, one that is cut leaves (maximum, sum, output) of every
-// piece in the workspace and a second kernel joins them.  The shares follow from the lengths alone, so the order of all
-// sums, and the result, is the same in every run.
+// rows: the cache of all sequences and kv heads is one line of key tiles (an "item" = one sequence, one kv head, one tile
+// of query rows; its keys in tiles of 4 KB), and warp w of a grid that fills the GPU takes the w-th equal share of that
+// line, wherever the lengths put its ends.  A running maximum and sum per query row make one pass over the data enough;
+// an item that lies inside one share is written at once, one that is cut leaves (output, maximum, sum) of every piece in
+// the workspace: the CTA joins the pieces of its four warps, a second kernel those of several CTAs.  The shares follow
+// from the lengths alone, so the order of all sums, and the result, is the same in every run.
 //
-// Each warp streams its own keys of a block through its own ring of shared-memory stages with 16-byte asynchronous
-// copies, so the main loop has no barrier; the page of a key is looked up one stage before its copy is issued.
+// A warp streams its tiles through its own ring of shared-memory stages with 16-byte asynchronous copies that run ahead
+// over the ends of items, and the page of a key is looked up one tile before its copy is issued; nothing in the main loop
+// waits for another warp.  (Shares per CTA, with the four warps on the keys of one item, paid for a join at every item:
+// 128 sequences of 64 - 512 keys, 32 heads of 64 columns, took 137 us.)
 #include "../../include/t5_b200.h"
 #include "paged.cuh"
 
@@ -25,7 +27,8 @@
 namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kMaxCtas = 444;      // 148 SMs, at most 3 CTAs each
+constexpr int kMaxCtas = 296;      // 148 SMs, two CTAs each (the rings take 96 KB)
+constexpr int kMaxWorkers = kMaxCtas * kWarps;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttnParams {
@@ -41,17 +44,24 @@ struct AttnParams {
   int tiles;             // tiles of query rows per kv head: ceil(n_q m / RT)
   int cap;               // keys a page table row can name
   PagedPool pool;
-  float* part;           // [ctas][2][rows][d + 2]: output, maximum, sum of the cut pieces
-  int4* meta;            // [ctas]: see Piece
+  int runs;              // 1: pages hold whole runs of keys (KeyStream)
+  float* warp_part;      // [workers][2][rows][d + 2]: output, maximum, sum of the pieces a warp leaves
+  float* part;           // [ctas][2][rows][d + 2]: the same of a CTA
+  int4* meta;            // [ctas]: which pieces those are, see below
   int rows;              // query rows of a slot: min(RT, n_q m)
   int* status;
 };
 
-// What CTA c left in the workspace: item of its first / last piece (-1: none) and whether that piece goes on beyond it.
-//   x: item whose piece in slot 0 began in an earlier CTA (-1: none)     y: 1 if that piece goes on in the next CTA
-//   z: item whose piece in slot 1 began here and goes on in the next CTA (-1: none)
-// (one int4; the join reads the z of its own CTA and the x, y of those behind it)
+// What a share (of a warp, of a CTA) leaves of the items it cuts:
+//   x: item whose piece in slot 0 began in an earlier share (-1: none)   y: 1 if that item goes on in the next share
+//   z: item whose piece in slot 1 began here and goes on in the next share (-1: none)
 
+// 2^x, results below 2^-126 as zero (they are weights relative to the largest one)
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ int row_len(const AttnParams& a, int r) { return min(max(a.lens[r], 0), a.cap); }
 __device__ __forceinline__ int seq_len(const AttnParams& a, int s) {      // keys any row of the sequence sees
   int n = 0;
@@ -79,13 +89,13 @@ __device__ __forceinline__ void step(const AttnParams& a, int bk, Place& p) {
   if (++p.s < a.S) { p.len = seq_len(a, p.s); p.nb = blocks_of(p.len, bk); }
 }
 
-// This CTA's share [x0, x1) of the line and the place of x0.  Called by all threads.
+// This warp's share [x0, x1) of the line and the place of x0.  Called by all threads.
 __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1, Place& p) {
   __shared__ int64_t sums[kWarps];
-  __shared__ int64_t found_prefix;
-  __shared__ int found_s;
+  __shared__ int64_t found_prefix[kWarps];
+  __shared__ int found_s[kWarps];
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-  int64_t mine = 0;      // blocks per item of this thread's sequences
+  int64_t mine = 0;      // tiles per item of this thread's sequences
   int first = 0;
   for (int s = tid; s < a.S; s += kThreads) {
     const int n = blocks_of(seq_len(a, s), bk);
@@ -98,14 +108,18 @@ __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1
   int64_t total = 0;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) total += sums[i];
-  const int64_t items = (int64_t)a.G * a.tiles;
+  const int64_t items = (int64_t)a.G * a.tiles, n_w = (int64_t)gridDim.x * kWarps;
   total *= items;
-  const int64_t c = blockIdx.x, n = gridDim.x;
-  if (total >= n) { x0 = total * c / n; x1 = total * (c + 1) / n; }
-  else { x0 = min(c, total); x1 = min(c + 1, total); }      // the CTAs without work lie behind all others
-  if (x0 == x1) return;
-  // the sequence whose blocks hold x0: prefix(s) <= x0 / items < prefix(s + 1)
-  const int64_t at = x0 / items;
+  int64_t at[kWarps];      // where the warps' shares begin, in tiles of one item per sequence (-1: no share)
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    const int64_t c = (int64_t)blockIdx.x * kWarps + i;
+    // fewer tiles than warps: the warps without work lie behind all others
+    const int64_t b0 = total >= n_w ? total * c / n_w : min(c, total), b1 = total >= n_w ? total * (c + 1) / n_w : min(c + 1, total);
+    at[i] = b0 < b1 ? b0 / items : -1;
+    if (i == w) { x0 = b0; x1 = b1; }
+  }
+  // the sequence whose tiles hold x0: prefix(s) <= x0 / items < prefix(s + 1)
   int64_t base = 0;
   for (int s0 = 0; s0 < a.S; s0 += kThreads) {
     const int s = s0 + tid;
@@ -119,21 +133,23 @@ __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1
     __syncthreads();
     if (lane == 31) sums[w] = inc;
     __syncthreads();
-    int64_t before = base + inc - n, all = base;
+    int64_t before = base + inc - n;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) {
       if (i < w) before += sums[i];
-      all += sums[i];
+      base += sums[i];
     }
-    if (n > 0 && before <= at && at < before + n) { found_s = s; found_prefix = before; }
-    base = all;
-    if (at < base) break;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i)
+      if (at[i] >= before && at[i] < before + n) { found_s[i] = s; found_prefix[i] = before; }
+    if (at[kWarps - 1] >= 0 ? at[kWarps - 1] < base : at[0] < base && at[1] < base && at[2] < base) break;
   }
   __syncthreads();
-  p.s = found_s;
+  if (x0 == x1) return;
+  p.s = found_s[w];
   p.len = seq_len(a, p.s);
   p.nb = blocks_of(p.len, bk);
-  const int64_t in = x0 - found_prefix * items;
+  const int64_t in = x0 - found_prefix[w] * items;
   p.k = (int)(in / p.nb);
   p.blk = (int)(in - (int64_t)p.k * p.nb);
 }
@@ -164,53 +180,81 @@ __device__ __forceinline__ int64_t key_offset(const AttnParams& a, const Place& 
 }
 
 // Shape of a warp's tiles: KT keys of DK columns of ES bytes, K then V, in a ring of STAGES.  4 KB of each where 32 lanes
-// can name the keys.  Measured with 2, 3 and 4 stages: three are within 1 % of four and leave room for a second CTA.
+// can name the keys.  A run of keys lies in one page when the page size is a multiple of it.
 template <int ES, int DK> struct Tile {
   static constexpr int ROW = DK * ES, CPR = ROW / 16;
   static constexpr int KT = 4096 / ROW < 32 ? 4096 / ROW : 32;
-  static constexpr int BK = KT * kWarps;
+  static constexpr int RUN = KT < 16 ? KT : 16, NR = KT / RUN;
   static constexpr int BYTES = KT * ROW, STAGES = 3;
   static constexpr int RING = STAGES * 2 * BYTES;
 };
 
-// A warp's stream of tiles: runs ahead of the arithmetic by STAGES - 1 tiles, over the ends of items.
+// A warp's stream of tiles: runs ahead of the arithmetic by STAGES - 1 tiles, over the ends of items.  Two ways to find
+// the keys of a tile: with pages of whole runs one look-up per run, the rows behind it by their stride; otherwise one per
+// key, passed between lanes.
 template <typename L> struct KeyStream {
   const AttnParams& a;
   Place at;             // of the next tile to be copied
-  int64_t left;         // tiles still to be copied
-  int64_t off;          // this lane's key of that tile: its page has been looked up one step ahead
+  int left;             // tiles still to be copied
+  int64_t off;          // this lane's run or key of that tile: its page has been looked up one step ahead
   unsigned char* ring;
   uint32_t ring_s;
   uint32_t* vmask;      // per stage: which keys of the tile exist
-  int w, lane;
+  int lane;
 
   __device__ __forceinline__ void lookup() {
-    off = left > 0 && lane < L::KT ? key_offset(a, at, at.blk * L::BK + w * L::KT + lane) : -1;
+    off = -1;
+    if (left > 0 && lane < (a.runs ? L::NR : L::KT)) off = key_offset(a, at, at.blk * L::KT + lane * (a.runs ? L::RUN : 1));
   }
   __device__ __forceinline__ void issue(int stage) {
     if (left > 0) {
-      const uint32_t ok = __ballot_sync(0xffffffffu, off >= 0);
-      if (lane == 0) vmask[stage] = ok;
+      constexpr int RPI = 32 / L::CPR;      // rows one instruction of the warp covers
+      const int c = lane % L::CPR, r0 = lane / L::CPR;
       const uint32_t kd = ring_s + stage * 2 * L::BYTES, vd = kd + L::BYTES;
-      const int c = lane % L::CPR;
+      uint32_t ok = __ballot_sync(0xffffffffu, off >= 0);
+      if (a.runs) {
+        const int n = at.len - at.blk * L::KT;      // keys of the sequence from here on
+        uint32_t have = 0;
 #pragma unroll
-      for (int i = 0; i < L::KT * L::CPR / 32; ++i) {
-        const int row = lane / L::CPR + i * (32 / L::CPR);
-        const int64_t o = __shfl_sync(0xffffffffu, off, row);
-        const uint32_t d = row * L::ROW + swz<L::CPR>(row, c) * 16;
-        const int64_t src = o >= 0 ? o + c * 16 : 0;
-        cp_async16(kd + d, a.pool.k + src, o >= 0);      // a key that does not exist becomes zeros
-        cp_async16(vd + d, a.pool.v + src, o >= 0);
+        for (int i = 0; i < L::NR; ++i) have |= ((ok >> i) & 1) ? ((1u << L::RUN) - 1u) << (i * L::RUN) : 0u;
+        if (n < L::KT) have &= (1u << max(n, 0)) - 1u;
+        ok = have;
+        const int64_t dv = (intptr_t)a.pool.v - (intptr_t)a.pool.k;
+#pragma unroll
+        for (int run = 0; run < L::NR; ++run) {
+          const int64_t o = __shfl_sync(0xffffffffu, off, run);
+          const char* src = a.pool.k + (o >= 0 ? o : 0) + r0 * a.pool.slot_stride + c * 16;
+#pragma unroll
+          for (int i = run * (L::RUN / RPI); i < (run + 1) * (L::RUN / RPI); ++i) {
+            const int row = r0 + i * RPI;
+            const uint32_t d = row * L::ROW + swz<L::CPR>(row, c) * 16;
+            const bool in = (ok >> row) & 1;
+            cp_async16(kd + d, src, in);      // a key that does not exist becomes zeros
+            cp_async16(vd + d, src + dv, in);
+            src += RPI * a.pool.slot_stride;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < L::KT / RPI; ++i) {
+          const int row = r0 + i * RPI;
+          const int64_t o = __shfl_sync(0xffffffffu, off, row);
+          const uint32_t d = row * L::ROW + swz<L::CPR>(row, c) * 16;
+          const int64_t src = o >= 0 ? o + c * 16 : 0;
+          cp_async16(kd + d, a.pool.k + src, o >= 0);
+          cp_async16(vd + d, a.pool.v + src, o >= 0);
+        }
       }
-      step(a, L::BK, at);
+      if (lane == 0) vmask[stage] = ok;
+      step(a, L::KT, at);
       --left;
     }
     cp_async_commit();
     lookup();
   }
   __device__ __forceinline__ KeyStream(const AttnParams& p, const Place& from, int64_t n, unsigned char* r, uint32_t* vm,
-                                       int warp, int ln)
-      : a(p), at(from), left(n), ring(r), ring_s((uint32_t)__cvta_generic_to_shared(r)), vmask(vm), w(warp), lane(ln) {
+                                       int ln)
+      : a(p), at(from), left((int)n), ring(r), ring_s((uint32_t)__cvta_generic_to_shared(r)), vmask(vm), lane(ln) {
     lookup();
 #pragma unroll
     for (int i = 0; i < L::STAGES - 1; ++i) issue(i);
@@ -226,45 +270,10 @@ struct Rows {
   __device__ __forceinline__ int head(const AttnParams& a, int r) const { return g * a.m + (r0 + r) % a.m; }
 };
 
-// End of an item or of the share: joins the warps' rows [from, from + MR) (merge [warp][MR][DK + 2]: output, maximum, sum;
-// written by the caller) and writes the finished rows, or the piece.  Called by all threads.  A few rows at a time keep
-// the buffer small enough for two CTAs per SM.
-template <typename T, int DK, int RT, int MR>
-__device__ __forceinline__ void finish_rows(const AttnParams& a, const Place& p, const float* merge, bool whole, int slot,
-                                            int from) {
-  __syncthreads();
-  const Rows rows(a, p, RT);
-  for (int idx = threadIdx.x; idx < min(rows.n - from, MR) * DK; idx += kThreads) {
-    const int mr = idx / DK, c = idx % DK, r = from + mr;
-    float mx = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) mx = fmaxf(mx, merge[(i * MR + mr) * (DK + 2) + DK]);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    float acc = 0.f, sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      const float* mg = merge + (i * MR + mr) * (DK + 2);
-      const float f = exp2f((mg[DK] - ref) * kLog2e);
-      acc += f * mg[c];
-      sum += f * mg[DK + 1];
-    }
-    if (whole) {
-      const int h = rows.head(a, r), row = rows.token(a, p, r);
-      reinterpret_cast<T*>(a.out + (int64_t)row * a.ldo)[h * DK + c] = from_f<T>(sum == 0.f ? 0.f : acc / sum);
-      if (c == 0 && a.lse != nullptr) a.lse[(int64_t)row * a.H + h] = sum == 0.f ? -INFINITY : mx + logf(sum);
-    } else {
-      float* pt = a.part + (((int64_t)blockIdx.x * 2 + slot) * a.rows + r) * (DK + 2);
-      pt[c] = acc;
-      if (c == 0) { pt[DK] = mx; pt[DK + 1] = sum; }
-    }
-  }
-  __syncthreads();
-}
-
-// Bookkeeping of a CTA's walk over its share: which piece an item's end leaves where (see AttnParams::meta)
+// Bookkeeping of a walk over a share: which piece an item's end leaves where
 struct Pieces {
   int4 meta = make_int4(-1, 0, -1, 0);
-  bool starts_here;
+  bool starts_here = true;
   __device__ __forceinline__ bool whole(bool item_ends) const { return item_ends && starts_here; }
   __device__ __forceinline__ int slot() const { return starts_here ? 1 : 0; }
   __device__ __forceinline__ void note(const AttnParams& a, const Place& p, bool item_ends) {
@@ -277,6 +286,85 @@ struct Pieces {
   }
 };
 
+// Where the rows of an item go
+__device__ __forceinline__ Place item_place(const AttnParams& a, int item) {
+  Place p;
+  p.s = item / (a.G * a.tiles); p.k = item % (a.G * a.tiles); p.blk = p.nb = p.len = 0;
+  return p;
+}
+template <typename T, int DK>
+__device__ __forceinline__ T* out_row(const AttnParams& a, int row, int h) {
+  return reinterpret_cast<T*>(a.out + (int64_t)row * a.ldo) + h * DK;
+}
+__device__ __forceinline__ void write_lse(const AttnParams& a, int row, int h, float mx, float sum) {
+  if (a.lse != nullptr) a.lse[(int64_t)row * a.H + h] = sum == 0.f ? -INFINITY : mx + logf(sum);
+}
+
+// End of a CTA: joins the pieces its warps left.  A chain of them that begins and ends here is an item's rows; one that
+// reaches beyond this CTA's first or last warp becomes the CTA's piece.  Chain w (-1: the one that comes in from the CTA
+// before) is taken by warp (w + 1) % 4.  Called by all threads.
+template <typename T, int DK, int RT>
+__device__ void finish_cta(const AttnParams& a, const int4& mine) {
+  __shared__ int4 metas[kWarps];
+  const int tid = threadIdx.x, lane = tid & 31;
+  if (lane == 0) metas[tid >> 5] = mine;
+  __syncthreads();      // also orders the warps' pieces in global memory before the reads below
+  constexpr int VC = DK / 32;
+  const int64_t piece = (int64_t)a.rows * (DK + 2);
+  const float* parts = a.warp_part + (int64_t)blockIdx.x * kWarps * 2 * piece;
+  if (tid == 0) a.meta[blockIdx.x] = make_int4(metas[0].x, 0, -1, 0);
+  __syncthreads();
+  for (int w = (tid >> 5) - 1; w < kWarps; w += kWarps) {
+    // the chain that begins with warp w's slot 1, or (w = -1) with the first warp's slot 0
+    const int item = w < 0 ? metas[0].x : metas[w].z;
+    if (item < 0) continue;
+    int end = w < 0 ? 0 : w;
+    bool goes_on = w < 0 ? metas[0].y != 0 : true;
+    while (goes_on && end + 1 < kWarps) goes_on = metas[++end].y != 0;
+    const int n = end - w + (w < 0 ? 0 : 1);      // pieces: w < 0: slots 0 of warps 0 .. end; else slot 1 of w, slots 0 behind it
+    const bool whole = w >= 0 && !goes_on;
+    if (lane == 0 && goes_on) (w < 0 ? a.meta[blockIdx.x].y : a.meta[blockIdx.x].z) = w < 0 ? 1 : item;
+    const Place p = item_place(a, item);
+    const Rows rows(a, p, RT);
+    const float* first = parts + (w < 0 ? 0 : 2 * w + 1) * piece;
+    const int64_t second = w < 0 ? 2 * piece : piece;      // from the first piece to the one behind it; then 2 piece
+#pragma unroll 4
+    for (int r = 0; r < rows.n; ++r) {
+      float mx = -INFINITY, sum = 0.f, pm[kWarps], acc[VC];
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        const float* q = first + (i == 0 ? 0 : second + (i - 1) * 2 * piece) + r * (DK + 2);
+        pm[i] = i < n ? q[DK] : -INFINITY;
+        mx = fmaxf(mx, pm[i]);
+      }
+      const float ref = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+      for (int c = 0; c < VC; ++c) acc[c] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        const float* q = first + (i == 0 ? 0 : second + (i - 1) * 2 * piece) + r * (DK + 2);
+        const float e = ex2((pm[i] - ref) * kLog2e);
+        if (i < n) {
+          sum += e * q[DK + 1];
+#pragma unroll
+          for (int c = 0; c < VC; ++c) acc[c] += e * q[lane + 32 * c];
+        }
+      }
+      if (whole) {
+        const int h = rows.head(a, r), row = rows.token(a, p, r);
+#pragma unroll
+        for (int c = 0; c < VC; ++c) out_row<T, DK>(a, row, h)[lane + 32 * c] = from_f<T>(sum == 0.f ? 0.f : acc[c] / sum);
+        if (lane == 0) write_lse(a, row, h, mx, sum);
+      } else {
+        float* pt = a.part + ((int64_t)blockIdx.x * 2 + (w < 0 ? 0 : 1)) * piece + r * (DK + 2);
+#pragma unroll
+        for (int c = 0; c < VC; ++c) pt[lane + 32 * c] = acc[c];
+        if (lane == 0) { pt[DK] = mx; pt[DK + 1] = sum; }
+      }
+    }
+  }
+}
+
 __device__ __forceinline__ void report_length(const AttnParams& a, int row) {
   if (a.lens[row] > a.cap) paged_report(a.status, PAGED_BAD_LENGTH);
 }
@@ -287,31 +375,26 @@ template <int DK, int RT> struct Simt : Tile<4, DK> {
   using B = Tile<4, DK>;
   static constexpr int PARTS = 32 / B::KT, CL = B::CPR / PARTS;      // lanes per key, chunks per lane
   static constexpr int VC = DK / 32;                                 // output columns per lane
-  static constexpr int QS = RT * DK * 4;                             // query rows of the item
-  static constexpr int MR = RT < 4 ? RT : 4;
-  static constexpr int SMEM = kWarps * (B::RING + B::STAGES * 4) + QS + kWarps * MR * (DK + 2) * 4;
+  static constexpr int QS = RT * DK * 4;                             // query rows of a warp's item
+  static constexpr int SMEM = kWarps * (B::RING + QS + B::STAGES * 4);
 };
 
 template <int DK, int RT>
-__global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_constant__ AttnParams a) {
+__global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __grid_constant__ AttnParams a) {
   pdl_sync();
   using L = Simt<DK, RT>;
   extern __shared__ __align__(128) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-  float* qs = reinterpret_cast<float*>(smem + kWarps * L::RING);
-  uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * L::RING + L::QS) + w * L::STAGES;
-  float* merge = reinterpret_cast<float*>(smem + kWarps * (L::RING + L::STAGES * 4) + L::QS);
+  float* qs = reinterpret_cast<float*>(smem + kWarps * L::RING + w * L::QS);
+  uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * (L::RING + L::QS)) + w * L::STAGES;
 
   int64_t x0, x1;
-  Place cur;
-  find_share(a, L::BK, x0, x1, cur);
+  Place cur = {};
+  find_share(a, L::KT, x0, x1, cur);
   Pieces pieces;
-  if (x0 == x1) {
-    if (tid == 0) a.meta[blockIdx.x] = pieces.meta;
-    return;
-  }
   pieces.starts_here = cur.blk == 0;
-  KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, w, lane);
+  float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * (DK + 2);
+  KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, lane);
 
   const int key_l = lane % L::KT, part_l = lane / L::KT;
   float m[RT], l[RT], o[RT][L::VC];
@@ -323,7 +406,8 @@ __global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_
     const int nr = rows.n;
     if (fresh) {
       fresh = false;
-      for (int idx = tid; idx < RT * DK; idx += kThreads) {
+      __syncwarp();
+      for (int idx = lane; idx < RT * DK; idx += 32) {
         const int r = idx / DK;
         qs[idx] = r < nr ? reinterpret_cast<const float*>(a.q + (int64_t)rows.token(a, cur, r) * a.ldq)[rows.head(a, r) * DK + idx % DK] : 0.f;
       }
@@ -334,13 +418,12 @@ __global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_
 #pragma unroll
         for (int c = 0; c < L::VC; ++c) o[r][c] = 0.f;
       }
-      if (tid < nr) report_length(a, rows.token(a, cur, tid));
-      __syncthreads();      // the last item's reads of qs lie before the barriers of finish_rows
+      if (lane < nr) report_length(a, rows.token(a, cur, lane));
     }
     cp_async_wait<L::STAGES - 2>();
     __syncwarp();
     keys.issue((stage + L::STAGES - 1) % L::STAGES);
-    const int j0 = cur.blk * L::BK + w * L::KT, j = j0 + key_l;
+    const int j0 = cur.blk * L::KT, j = j0 + key_l;
     const uint32_t ok = vmask[stage];
     if (ok != 0) {
       const unsigned char* kt = keys.ring + stage * 2 * L::BYTES;
@@ -375,8 +458,8 @@ __global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_
           for (int of = 16; of > 0; of >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, of));
           mx = fmaxf(m[r], mx);
           const float ref = mx == -INFINITY ? 0.f : mx;
-          const float corr = exp2f((m[r] - ref) * kLog2e);
-          const float p = exp2f((s - ref) * kLog2e);
+          const float corr = ex2((m[r] - ref) * kLog2e);
+          const float p = ex2((s - ref) * kLog2e);
           m[r] = mx;
           l[r] = l[r] * corr + p;
           sc[r] = p;
@@ -407,29 +490,29 @@ __global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_
     const bool item_ends = cur.blk + 1 == cur.nb;
     if (item_ends || x + 1 == x1) {
 #pragma unroll
-      for (int from = 0; from < RT; from += L::MR) {
-        if (from < nr) {
+      for (int r = 0; r < RT; ++r) {
+        if (r < nr) {
+          float lt = part_l == 0 ? l[r] : 0.f;
 #pragma unroll
-          for (int mr = 0; mr < L::MR; ++mr) {
-            const int r = from + mr;
-            float lt = part_l == 0 ? l[r] : 0.f;
+          for (int of = 16; of > 0; of >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
+          const bool whole = pieces.whole(item_ends);
+          const int h = rows.head(a, r), row = rows.token(a, cur, r);
+          float* at = whole ? out_row<float, DK>(a, row, h) : part + (pieces.slot() * a.rows + r) * (DK + 2);
 #pragma unroll
-            for (int of = 16; of > 0; of >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
-            float* mg = merge + (w * L::MR + mr) * (DK + 2);
-#pragma unroll
-            for (int c = 0; c < L::VC; ++c) mg[lane * L::VC + c] = o[r][c];
-            if (lane == 0) { mg[DK] = m[r]; mg[DK + 1] = lt; }
+          for (int c = 0; c < L::VC; ++c) at[lane * L::VC + c] = !whole ? o[r][c] : (lt == 0.f ? 0.f : o[r][c] / lt);
+          if (lane == 0) {
+            if (whole) write_lse(a, row, h, m[r], lt);
+            else { at[DK] = m[r]; at[DK + 1] = lt; }
           }
-          finish_rows<float, DK, RT, L::MR>(a, cur, merge, pieces.whole(item_ends), pieces.slot(), from);
         }
       }
       pieces.note(a, cur, item_ends);
       fresh = true;
     }
-    step(a, L::BK, cur);
+    step(a, L::KT, cur);
   }
   cp_async_wait<0>();
-  if (tid == 0) a.meta[blockIdx.x] = pieces.meta;
+  finish_cta<float, DK, RT>(a, pieces.meta);
 }
 
 // ------------------------------------------------------------------ bfloat16: matrix instructions
@@ -442,7 +525,7 @@ __global__ void __launch_bounds__(kThreads) paged_attn_simt_kernel(const __grid_
 // instructions per 16 keys, on a pipe that has the room), so the output is the float32 result rounded once.
 template <int DK, int RT> struct Mma : Tile<2, DK> {
   using B = Tile<2, DK>;
-  static constexpr int SMEM = kWarps * (B::RING + B::STAGES * 4) + kWarps * 8 * (DK + 2) * 4;
+  static constexpr int SMEM = kWarps * (B::RING + B::STAGES * 4);
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
@@ -474,8 +557,29 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t&
   lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 
+__device__ __forceinline__ bool not_finite(uint32_t two) {      // either bfloat16 has an exponent of all ones
+  return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
+}
+// O += P V of one tile without a product that a row does not see: s, o as in the kernel, rows see the first n0 / n1 keys
 template <int DK, int RT>
-__global__ void __launch_bounds__(kThreads) paged_attn_mma_kernel(const __grid_constant__ AttnParams a) {
+__device__ __noinline__ void values_by_key(const unsigned char* vt, const float* s, float* o, int n0, int n1) {
+  using L = Mma<DK, RT>;
+  constexpr int CN = RT / 4;
+  const int lane = threadIdx.x & 31, quad = lane & 3;
+  for (int kk = 0; kk < L::KT; ++kk)
+    for (int hf = 0; hf < RT / 8; ++hf) {
+      const float p = __shfl_sync(0xffffffffu, s[(kk / 8) * CN + 2 * hf + (kk & 1)], (lane & ~3) | ((kk & 7) >> 1));
+      if (kk < (hf ? n1 : n0))
+        for (int t = 0; t < DK / 8; ++t) {
+          const uint32_t u = *reinterpret_cast<const uint32_t*>(vt + kk * L::ROW + swz<L::CPR>(kk, t) * 16 + quad * 4);
+          o[t * CN + 2 * hf] = fmaf(p, __uint_as_float(u << 16), o[t * CN + 2 * hf]);
+          o[t * CN + 2 * hf + 1] = fmaf(p, __uint_as_float(u & 0xffff0000u), o[t * CN + 2 * hf + 1]);
+        }
+    }
+}
+
+template <int DK, int RT>
+__global__ void __launch_bounds__(kThreads, 2) paged_attn_mma_kernel(const __grid_constant__ AttnParams a) {
   pdl_sync();
   using L = Mma<DK, RT>;
   constexpr bool H16 = RT == 16;
@@ -484,18 +588,14 @@ __global__ void __launch_bounds__(kThreads) paged_attn_mma_kernel(const __grid_c
   extern __shared__ __align__(128) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, quad = lane & 3;
   uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * L::RING) + w * L::STAGES;
-  float* merge = reinterpret_cast<float*>(smem + kWarps * (L::RING + L::STAGES * 4));
 
   int64_t x0, x1;
-  Place cur;
-  find_share(a, L::BK, x0, x1, cur);
+  Place cur = {};
+  find_share(a, L::KT, x0, x1, cur);
   Pieces pieces;
-  if (x0 == x1) {
-    if (tid == 0) a.meta[blockIdx.x] = pieces.meta;
-    return;
-  }
   pieces.starts_here = cur.blk == 0;
-  KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, w, lane);
+  float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * (DK + 2);
+  KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, lane);
 
   uint32_t qf[KS][2 * NH];               // A operand: columns 16 ks + 2 quad (+ 8), rows lane / 4 (+ 8)
   float m[NH], l[NH], o[NT][CN], far[NH];
@@ -533,12 +633,12 @@ __global__ void __launch_bounds__(kThreads) paged_attn_mma_kernel(const __grid_c
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < CN; ++i) o[t][i] = 0.f;
-      if (tid < rows.n) report_length(a, rows.token(a, cur, tid));
+      if (lane < rows.n) report_length(a, rows.token(a, cur, lane));
     }
     cp_async_wait<L::STAGES - 2>();
     __syncwarp();
     keys.issue((stage + L::STAGES - 1) % L::STAGES);
-    const int j0 = cur.blk * L::BK + w * L::KT;
+    const int j0 = cur.blk * L::KT;
     const uint32_t ok = vmask[stage];
     if (ok != 0) {
       const uint32_t kt = keys.ring_s + stage * 2 * L::BYTES, vt = kt + L::BYTES;
@@ -567,18 +667,28 @@ __global__ void __launch_bounds__(kThreads) paged_attn_mma_kernel(const __grid_c
 #pragma unroll
       for (int t = 0; t < NG * 2; ++t)
 #pragma unroll
-        for (int i = 0; i < CN; ++i) {
-          const int hf = i >> 1, kk = t * 8 + quad * 2 + (i & 1);
-          float v = s[t][i] * a.scale;
-          if (near) {
-            if (bias[hf] != nullptr && j0 + kk < len[hf]) v += bias[hf][max(a.n_bias - len[hf] + j0 + kk, 0)];
-          } else {
-            v += far[hf];
+        for (int i = 0; i < CN; ++i) s[t][i] = fmaf(s[t][i], a.scale, near ? 0.f : far[i >> 1]);
+      if (near) {
+#pragma unroll
+        for (int t = 0; t < NG * 2; ++t)
+#pragma unroll
+          for (int i = 0; i < CN; ++i) {
+            const int hf = i >> 1, j = j0 + t * 8 + quad * 2 + (i & 1);
+            if (j < len[hf]) s[t][i] += bias[hf][max(a.n_bias - len[hf] + j, 0)];
           }
-          if (!all_seen && !(((ok >> kk) & 1) && j0 + kk < len[hf])) v = -INFINITY;
-          s[t][i] = v;
-          top[hf] = fmaxf(top[hf], v);
-        }
+      }
+      if (!all_seen) {
+        const uint32_t mine = ok >> (quad * 2);
+#pragma unroll
+        for (int t = 0; t < NG * 2; ++t)
+#pragma unroll
+          for (int i = 0; i < CN; ++i)
+            if (!((mine >> (t * 8 + (i & 1))) & 1) || j0 + t * 8 + quad * 2 + (i & 1) >= len[i >> 1]) s[t][i] = -INFINITY;
+      }
+#pragma unroll
+      for (int t = 0; t < NG * 2; ++t)
+#pragma unroll
+        for (int i = 0; i < CN; ++i) top[i >> 1] = fmaxf(top[i >> 1], s[t][i]);
       float ref[NH];
       bool moved = false;
 #pragma unroll
@@ -591,7 +701,7 @@ __global__ void __launch_bounds__(kThreads) paged_attn_mma_kernel(const __grid_c
       if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
         for (int hf = 0; hf < NH; ++hf) {
-          const float corr = exp2f((m[hf] - ref[hf]) * kLog2e);
+          const float corr = ex2((m[hf] - ref[hf]) * kLog2e);
           l[hf] *= corr;
           m[hf] = top[hf];
 #pragma unroll
@@ -603,22 +713,18 @@ __global__ void __launch_bounds__(kThreads) paged_attn_mma_kernel(const __grid_c
 #pragma unroll
         for (int i = 0; i < CN; ++i) {
           const int hf = i >> 1;
-          s[t][i] = exp2f((s[t][i] - ref[hf]) * kLog2e);      // differences first: a bias of the lowest float stays finite
+          s[t][i] = ex2((s[t][i] - ref[hf]) * kLog2e);      // differences first: a bias of the lowest float stays finite
           l[hf] += s[t][i];
         }
       // Keys that one row sees and another does not have weight 0 there, and 0 x NaN would spoil the row: if such a tile
       // holds a value that is not finite, it is taken key by key.
       bool plain = false;
-      if (j0 + L::KT > min_len) {
+      if (min_len < min(j0 + L::KT, cur.len)) {
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < L::BYTES / 512; ++i) {
-          uint32_t u[4];
-          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                       : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(vt + (i * 32 + lane) * 16) : "memory");
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            bad |= (u[k] & 0x7f80u) == 0x7f80u || (u[k] & 0x7f800000u) == 0x7f800000u;
+          const uint4 u = *reinterpret_cast<const uint4*>(keys.ring + stage * 2 * L::BYTES + L::BYTES + (i * 32 + lane) * 16);
+          bad |= not_finite(u.x) | not_finite(u.y) | not_finite(u.z) | not_finite(u.w);
         }
         plain = __any_sync(0xffffffffu, bad);
       }
@@ -644,63 +750,66 @@ __global__ void __launch_bounds__(kThreads) paged_attn_mma_kernel(const __grid_c
           }
         }
       } else {
+        // copies, so that the rare call below does not push the registers of the others into memory
+        float sc[NG * 2 * CN], oc[NT * CN];
 #pragma unroll
-        for (int kk = 0; kk < L::KT; ++kk) {
+        for (int i = 0; i < NG * 2 * CN; ++i) sc[i] = s[i / CN][i % CN];
 #pragma unroll
-          for (int hf = 0; hf < NH; ++hf) {
-            const float p = __shfl_sync(0xffffffffu, s[kk / 8][2 * hf + (kk & 1)], (lane & ~3) | ((kk & 7) >> 1));
-            if (j0 + kk < len[hf]) {
-#pragma unroll 1
-              for (int t = 0; t < NT; ++t) {
-                uint32_t u;
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u) : "r"(vt + kk * L::ROW + swz<L::CPR>(kk, t) * 16 + quad * 4) : "memory");
-                const float v0 = __uint_as_float(u << 16), v1 = __uint_as_float(u & 0xffff0000u);
+        for (int i = 0; i < NT * CN; ++i) oc[i] = o[i / CN][i % CN];
+        values_by_key<DK, RT>(keys.ring + stage * 2 * L::BYTES + L::BYTES, sc, oc, len[0] - j0, len[NH - 1] - j0);
 #pragma unroll
-                for (int tt = 0; tt < NT; ++tt)      // o is indexed by constants only: it stays in registers
-                  if (tt == t) { o[tt][2 * hf] = fmaf(p, v0, o[tt][2 * hf]); o[tt][2 * hf + 1] = fmaf(p, v1, o[tt][2 * hf + 1]); }
-              }
-            }
-          }
-        }
+        for (int i = 0; i < NT * CN; ++i) o[i / CN][i % CN] = oc[i];
       }
     }
     stage = (stage + 1) % L::STAGES;
     const bool item_ends = cur.blk + 1 == cur.nb;
     if (item_ends || x + 1 == x1) {
-      const int n = Rows(a, cur, RT).n;
+      const Rows rows(a, cur, RT);
+      const bool whole = pieces.whole(item_ends);
 #pragma unroll
       for (int hf = 0; hf < NH; ++hf) {
         float lt = l[hf];
         lt += __shfl_xor_sync(0xffffffffu, lt, 1);
         lt += __shfl_xor_sync(0xffffffffu, lt, 2);
-        if (8 * hf + lane / 4 < n) {
-          float* mg = merge + (w * 8 + lane / 4) * (DK + 2);
+        const int r = lane / 4 + 8 * hf;
+        if (r < rows.n) {
+          if (whole) {
+            const int h = rows.head(a, r), row = rows.token(a, cur, r);
+            bf16* at = out_row<bf16, DK>(a, row, h) + quad * 2;
+            const float inv = lt == 0.f ? 0.f : 1.f / lt;
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-            *reinterpret_cast<float2*>(mg + t * 8 + quad * 2) = make_float2(o[t][2 * hf], o[t][2 * hf + 1]);
-          if (quad == 0) { mg[DK] = m[hf]; mg[DK + 1] = lt; }
+            for (int t = 0; t < NT; ++t)
+              *reinterpret_cast<__nv_bfloat162*>(at + t * 8) = __floats2bfloat162_rn(o[t][2 * hf] * inv, o[t][2 * hf + 1] * inv);
+            if (quad == 0) write_lse(a, row, h, m[hf], lt);
+          } else {
+            float* at = part + (pieces.slot() * a.rows + r) * (DK + 2);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+              *reinterpret_cast<float2*>(at + t * 8 + quad * 2) = make_float2(o[t][2 * hf], o[t][2 * hf + 1]);
+            if (quad == 0) { at[DK] = m[hf]; at[DK + 1] = lt; }
+          }
         }
-        if (8 * hf < n) finish_rows<bf16, DK, RT, 8>(a, cur, merge, pieces.whole(item_ends), pieces.slot(), 8 * hf);
       }
       pieces.note(a, cur, item_ends);
       fresh = true;
     }
-    step(a, L::BK, cur);
+    step(a, L::KT, cur);
   }
   cp_async_wait<0>();
-  if (tid == 0) a.meta[blockIdx.x] = pieces.meta;
+  finish_cta<bf16, DK, RT>(a, pieces.meta);
 }
 
-// Joins the pieces of the item that the boundary behind CTA blockIdx.x cuts first; one CTA per boundary and query row.
+// Joins the pieces of the item that the boundary behind CTA blockIdx.x is the first to cut; one CTA per boundary and query
+// row.
 template <typename T, int DK, int RT>
 __global__ void __launch_bounds__(128) paged_attn_join_kernel(const __grid_constant__ AttnParams a, int ctas) {
   pdl_sync();
   const int c0 = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int item = a.meta[c0].z;
   if (item < 0) return;
-  const int tile = (item % (a.G * a.tiles)) % a.tiles, g = (item % (a.G * a.tiles)) / a.tiles, s = item / (a.G * a.tiles);
-  const int rr = tile * RT + r;
-  if (rr >= a.n_q * a.m) return;
+  const Place p = item_place(a, item);
+  const Rows rows(a, p, RT);
+  if (r >= rows.n) return;
   // pieces: slot 1 of c0, then slot 0 of the CTAs behind it up to the one where the item ends (CTAs without work
   // lie behind all others)
   __shared__ int s_last;
@@ -725,7 +834,7 @@ __global__ void __launch_bounds__(128) paged_attn_join_kernel(const __grid_const
     const float* pt = piece(i);
     const float pm = pt[DK], ps = pt[DK + 1];
     const float nm = fmaxf(mx, pm), ref = nm == -INFINITY ? 0.f : nm;
-    const float f0 = exp2f((mx - ref) * kLog2e), f1 = exp2f((pm - ref) * kLog2e);
+    const float f0 = ex2((mx - ref) * kLog2e), f1 = ex2((pm - ref) * kLog2e);
     sum = sum * f0 + ps * f1;
 #pragma unroll
     for (int c = 0; c < VC; ++c) acc[c] = acc[c] * f0 + pt[lane * VC + c] * f1;
@@ -736,21 +845,19 @@ __global__ void __launch_bounds__(128) paged_attn_join_kernel(const __grid_const
   if (lane == 0) { red[w][DK] = mx; red[w][DK + 1] = sum; }
   __syncthreads();
   if (tid < DK) {
-    mx = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, red[i][DK]);
+    mx = fmaxf(fmaxf(red[0][DK], red[1][DK]), fmaxf(red[2][DK], red[3][DK]));
     const float ref = mx == -INFINITY ? 0.f : mx;
     float v = 0.f;
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float f = exp2f((red[i][DK] - ref) * kLog2e);
-      v += f * red[i][tid];
-      sum += f * red[i][DK + 1];
+      const float e = ex2((red[i][DK] - ref) * kLog2e);
+      v += e * red[i][tid];
+      sum += e * red[i][DK + 1];
     }
-    const int h = g * a.m + rr % a.m, row = s * a.n_q + rr / a.m;
-    reinterpret_cast<T*>(a.out + (int64_t)row * a.ldo)[h * DK + tid] = from_f<T>(sum == 0.f ? 0.f : v / sum);
-    if (tid == 0 && a.lse != nullptr) a.lse[(int64_t)row * a.H + h] = sum == 0.f ? -INFINITY : mx + logf(sum);
+    const int h = rows.head(a, r), row = rows.token(a, p, r);
+    out_row<T, DK>(a, row, h)[tid] = from_f<T>(sum == 0.f ? 0.f : v / sum);
+    if (tid == 0) write_lse(a, row, h, mx, sum);
   }
 }
 
@@ -782,6 +889,7 @@ cudaError_t grid_of(Kernel kernel, int smem, int* ctas) {
 template <typename T, int DK, int RT>
 cudaError_t run_attention(AttnParams& a, Kernel kernel, int smem, cudaStream_t st) {
   int ctas = 0;
+  a.runs = a.pool.page_size % Tile<sizeof(T), DK>::RUN == 0;
   cudaError_t e = grid_of<T, DK, RT>(kernel, smem, &ctas);
   if (e != cudaSuccess) return e;
   a.tiles = (a.n_q * a.m + RT - 1) / RT;
@@ -806,7 +914,7 @@ template <int DK> cudaError_t run_bf16(AttnParams& a, cudaStream_t st) {
 int64_t paged_attention_workspace(int n_rows, int n_q, int H, int Hkv, int d_kv) {
   (void)n_rows;
   const int64_t all = (int64_t)n_q * (H / Hkv), rows = all < 16 ? all : 16;
-  return kMaxCtas * (int64_t)sizeof(int4) + kMaxCtas * 2 * rows * (d_kv + 2) * 4;
+  return kMaxCtas * (int64_t)sizeof(int4) + (kMaxCtas + kMaxWorkers) * 2 * rows * (d_kv + 2) * 4;
 }
 
 cudaError_t launch_paged_attention(const PagedAttnArgs& g, cudaStream_t st) {
@@ -820,7 +928,9 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& g, cudaStream_t st) {
   a.cap = g.pool.max_pages * g.pool.page_size;
   a.pool = g.pool; a.status = g.status;
   a.meta = (int4*)g.workspace;
+  const int rows = a.n_q * a.m < 16 ? a.n_q * a.m : 16;
   a.part = (float*)((char*)g.workspace + kMaxCtas * sizeof(int4));
+  a.warp_part = a.part + (int64_t)kMaxCtas * 2 * rows * (g.d_kv + 2);
   if (g.dtype == DT_F32) return g.d_kv == 32 ? run_f32<32>(a, st) : g.d_kv == 64 ? run_f32<64>(a, st) : run_f32<128>(a, st);
   return g.d_kv == 32 ? run_bf16<32>(a, st) : g.d_kv == 64 ? run_bf16<64>(a, st) : run_bf16<128>(a, st);
 }
