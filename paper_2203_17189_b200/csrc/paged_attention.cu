@@ -157,6 +157,9 @@ __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -209,8 +212,11 @@ template <typename L> struct KeyStream {
   __device__ __forceinline__ void issue(int stage) {
     if (left > 0) {
       constexpr int RPI = 32 / L::CPR;      // rows one instruction of the warp covers
+      constexpr uint32_t kAll = L::KT == 32 ? 0xffffffffu : (1u << L::KT) - 1u;
       const int c = lane % L::CPR, r0 = lane / L::CPR;
-      const uint32_t kd = ring_s + stage * 2 * L::BYTES, vd = kd + L::BYTES;
+      // place of row r0 + i RPI, chunk c: the swizzle's row bits come in by one exclusive-or
+      const uint32_t kd = ring_s + stage * 2 * L::BYTES + r0 * L::ROW + swz<L::CPR>(r0, c) * 16;
+      auto place = [&](int i) { return (kd ^ (swz<L::CPR>(i * RPI, 0) * 16)) + i * RPI * L::ROW; };
       uint32_t ok = __ballot_sync(0xffffffffu, off >= 0);
       if (a.runs) {
         const int n = at.len - at.blk * L::KT;      // keys of the sequence from here on
@@ -219,30 +225,33 @@ template <typename L> struct KeyStream {
         for (int i = 0; i < L::NR; ++i) have |= ((ok >> i) & 1) ? ((1u << L::RUN) - 1u) << (i * L::RUN) : 0u;
         if (n < L::KT) have &= (1u << max(n, 0)) - 1u;
         ok = have;
-        const int64_t dv = (intptr_t)a.pool.v - (intptr_t)a.pool.k;
+        const int64_t dv = (intptr_t)a.pool.v - (intptr_t)a.pool.k, dr = RPI * a.pool.slot_stride;
 #pragma unroll
         for (int run = 0; run < L::NR; ++run) {
           const int64_t o = __shfl_sync(0xffffffffu, off, run);
           const char* src = a.pool.k + (o >= 0 ? o : 0) + r0 * a.pool.slot_stride + c * 16;
+          if (ok == kAll) {
 #pragma unroll
-          for (int i = run * (L::RUN / RPI); i < (run + 1) * (L::RUN / RPI); ++i) {
-            const int row = r0 + i * RPI;
-            const uint32_t d = row * L::ROW + swz<L::CPR>(row, c) * 16;
-            const bool in = (ok >> row) & 1;
-            cp_async16(kd + d, src, in);      // a key that does not exist becomes zeros
-            cp_async16(vd + d, src + dv, in);
-            src += RPI * a.pool.slot_stride;
+            for (int i = run * (L::RUN / RPI); i < (run + 1) * (L::RUN / RPI); ++i, src += dr) {
+              cp_async16(place(i), src);
+              cp_async16(place(i) + L::BYTES, src + dv);
+            }
+          } else {
+#pragma unroll
+            for (int i = run * (L::RUN / RPI); i < (run + 1) * (L::RUN / RPI); ++i, src += dr) {
+              const bool in = (ok >> (r0 + i * RPI)) & 1;
+              cp_async16(place(i), src, in);      // a key that does not exist becomes zeros
+              cp_async16(place(i) + L::BYTES, src + dv, in);
+            }
           }
         }
       } else {
 #pragma unroll
         for (int i = 0; i < L::KT / RPI; ++i) {
-          const int row = r0 + i * RPI;
-          const int64_t o = __shfl_sync(0xffffffffu, off, row);
-          const uint32_t d = row * L::ROW + swz<L::CPR>(row, c) * 16;
+          const int64_t o = __shfl_sync(0xffffffffu, off, r0 + i * RPI);
           const int64_t src = o >= 0 ? o + c * 16 : 0;
-          cp_async16(kd + d, a.pool.k + src, o >= 0);
-          cp_async16(vd + d, a.pool.v + src, o >= 0);
+          cp_async16(place(i), a.pool.k + src, o >= 0);
+          cp_async16(place(i) + L::BYTES, a.pool.v + src, o >= 0);
         }
       }
       if (lane == 0) vmask[stage] = ok;
@@ -600,14 +609,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_mma_kernel(const __gri
   uint32_t qf[KS][2 * NH];               // A operand: columns 16 ks + 2 quad (+ 8), rows lane / 4 (+ 8)
   float m[NH], l[NH], o[NT][CN], far[NH];
   const float* bias[NH];
-  int len[NH], min_len = 0;
+  int len[NH], min_len = 0, max_len = 0;      // keys this lane's rows see; over all rows
   bool fresh = true;
   int stage = 0;
   for (int64_t x = x0; x < x1; ++x) {
     if (fresh) {
       fresh = false;
       const Rows rows(a, cur, RT);
-      min_len = 0x7fffffff;
+      min_len = 0x7fffffff; max_len = 0;
 #pragma unroll
       for (int hf = 0; hf < NH; ++hf) {
         const int r = lane / 4 + 8 * hf;
@@ -617,7 +626,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_mma_kernel(const __gri
         if (valid) {
           const int row = rows.token(a, cur, r), h = rows.head(a, r);
           len[hf] = row_len(a, row);
-          min_len = min(min_len, len[hf]);
+          min_len = min(min_len, len[hf]); max_len = max(max_len, len[hf]);
           src = reinterpret_cast<const uint32_t*>(a.q + (int64_t)row * a.ldq + h * (DK * 2)) + quad;
           if (a.bias != nullptr) { bias[hf] = a.bias + (int64_t)h * a.n_bias; far[hf] = bias[hf][0]; }
         }
@@ -628,7 +637,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_mma_kernel(const __gri
         }
       }
 #pragma unroll
-      for (int of = 4; of < 32; of <<= 1) min_len = min(min_len, __shfl_xor_sync(0xffffffffu, min_len, of));
+      for (int of = 4; of < 32; of <<= 1) {
+        min_len = min(min_len, __shfl_xor_sync(0xffffffffu, min_len, of));
+        max_len = max(max_len, __shfl_xor_sync(0xffffffffu, max_len, of));
+      }
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -668,7 +680,16 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_mma_kernel(const __gri
       for (int t = 0; t < NG * 2; ++t)
 #pragma unroll
         for (int i = 0; i < CN; ++i) s[t][i] = fmaf(s[t][i], a.scale, near ? 0.f : far[i >> 1]);
-      if (near) {
+      if (near && all_seen && a.n_bias - max_len + j0 >= 0) {      // every distance of the tile has its entry
+#pragma unroll
+        for (int hf = 0; hf < NH; ++hf) {
+          if (bias[hf] != nullptr) {
+            const float* at = bias[hf] + (a.n_bias - len[hf] + j0 + quad * 2);
+#pragma unroll
+            for (int t = 0; t < NG * 2; ++t) { s[t][2 * hf] += at[t * 8]; s[t][2 * hf + 1] += at[t * 8 + 1]; }
+          }
+        }
+      } else if (near) {
 #pragma unroll
         for (int t = 0; t < NG * 2; ++t)
 #pragma unroll
