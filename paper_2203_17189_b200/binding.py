@@ -380,77 +380,86 @@ def t5_selftest_bounded_wait(status, limit_cycles):
     _check(lib().t5_selftest_bounded_wait(_ptr(status), int(limit_cycles), _stream()))
 
 
-# ---- serving.  A call here takes some microseconds on the GPU, so pointers and sizes go to ctypes as plain ints; what a
-# wrong tensor would turn into an access out of range (type, shape, place) is checked first.
+# ---- serving.  A call here takes some microseconds on the GPU, so the host side is kept to about as many: pointers and
+# sizes go to ctypes as plain ints, and what a wrong tensor would turn into an access out of range (type, shape, place) is
+# tested in one expression per call; only when that fails is the culprit looked for.
 
-def _require(ok, what):
-    if not ok:
-        raise T5Error(-8, what)
-
-
-def _dense(t, name, shape, dtype, device):
-    """A tensor of this shape, type and place whose last dimension is contiguous."""
-    if (t.dtype != dtype or t.device != device or t.shape != shape
-            or (shape[-1] > 1 and t.stride(-1) != 1)):
-        raise T5Error(-8, f"{name}: want a {dtype} tensor {shape} on {device} with a contiguous last dimension, "
-                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+_CODES = {torch.float32: 0, torch.bfloat16: 1}
+_I32, _F32 = torch.int32, torch.float32
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _heads(t, name, shape, dtype, device):
-    """[rows, heads, d_kv] whose rows are dense (a column slice of a wider matrix is fine); returns the row stride."""
-    _dense(t, name, shape, dtype, device)
-    _require(shape[1] == 1 or t.stride(1) == shape[2], f"{name}: heads must be adjacent columns")
-    return t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+def _refuse(device, checks):
+    """Raises for the first tensor that is not (name, tensor, dtype, shape) with a contiguous last dimension on the
+    current device."""
+    for name, t, dtype, shape in checks:
+        if t is None:
+            raise T5Error(-8, f"{name} is missing")
+        if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.get_device() != device or (
+                t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1):
+            raise T5Error(-8, f"{name}: want a {dtype} tensor {tuple(shape)} on the current device {device} with a contiguous "
+                              f"last dimension, got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+    raise T5Error(-8, "tensors: heads must be adjacent columns, both pools alike in their strides, vectors contiguous, all "
+                      "on the current CUDA device")
 
 
-def _place(t):
-    """(device, stream) of a call on this tensor; the device has to be the current one."""
-    _require(t.is_cuda and t.device.index == torch.cuda.current_device(), "tensors must lie on the current CUDA device")
-    return t.device, torch.cuda.current_stream().cuda_stream
+def _row_stride(t, shape, d):
+    """Row stride of [rows, heads, d] with adjacent heads, or -1; rows may be slices of wider ones."""
+    st = t.stride()
+    if st[2] != 1 or (st[1] != d and shape[1] > 1):
+        return -1
+    return st[0] if shape[0] > 1 else shape[1] * d
 
 
-def _dtype_code(t):
-    if t.dtype == torch.bfloat16:
-        return 1
-    _require(t.dtype == torch.float32, "want float32 or bfloat16")
-    return 0
-
-
-def _pool(k_pages, v_pages, table, device):
-    """Arguments that describe the page pools [n_pages, page_size, kv heads, d_kv] (any strides) and the page table."""
-    _require(k_pages.dim() == 4 and table.dim() == 2, "k_pages: want [n_pages, page_size, kv_heads, d_kv]; table: 2-D")
-    shape = tuple(k_pages.shape)
-    _dense(k_pages, "k_pages", shape, k_pages.dtype, device)
-    _dense(v_pages, "v_pages", shape, k_pages.dtype, device)
-    _dense(table, "page_table", tuple(table.shape), torch.int32, device)
+def _pool_strides(k_pages, v_pages, shape):
+    """Strides of both pools (a dimension of one entry has none), or None if they differ."""
+    sk, sv = k_pages.stride(), v_pages.stride()
+    if sk == sv and sk[3] == 1 and 1 not in shape:
+        return sk[0], sk[1], sk[2]
     n, ps, g, d = shape
-    st = [k_pages.stride(i) if shape[i] > 1 else ps * g * d for i in range(3)]      # a single entry has no stride
-    _require(all(v_pages.stride(i) == st[i] or shape[i] == 1 for i in range(3)), "k_pages and v_pages: same strides")
-    ld = table.stride(0) if table.shape[0] > 1 else table.shape[1]
-    return (k_pages.data_ptr(), v_pages.data_ptr(), n, ps, *st, table.data_ptr()), table.shape[1], ld
+    if sk[3] != 1 or sv[3] != 1 or any(sk[i] != sv[i] and shape[i] > 1 for i in range(3)):
+        return None
+    return tuple(sk[i] if shape[i] > 1 else ps * g * d for i in range(3))
 
 
 def t5_paged_kv_append(k, v, k_pages, v_pages, page_table, seq_of_token, positions, q=None, q_out=None, rot_dim=0,
                        rot_base=10000.0, rot_interleaved=False):
-    """k, v [tokens, kv_heads, d_kv] (and q [tokens, heads, d_kv] into q_out) enter the pools; see the header."""
-    device, stream = _place(k)
-    code = _dtype_code(k)
-    _require(k.dim() == 3 and k_pages.dim() == 4 and k_pages.dtype == k.dtype, "k: want [tokens, kv_heads, d_kv] of the pools' type")
-    n, g, d = k.shape
-    _require(tuple(k_pages.shape[2:]) == (g, d), "k_pages: heads or d_kv differ from k")
-    pool, max_pages, ld_table = _pool(k_pages, v_pages, page_table, device)
-    ldk, ldv = _heads(k, "k", (n, g, d), k.dtype, device), _heads(v, "v", (n, g, d), k.dtype, device)
-    _dense(seq_of_token, "seq_of_token", (n,), torch.int32, device)
-    _dense(positions, "positions", (n,), torch.int32, device)
+    """k, v [tokens, kv_heads, d_kv] (and q [tokens, heads, d_kv] into q_out) enter the pools [n_pages, page_size,
+    kv_heads, d_kv]; see the header."""
+    dt, dev = k.dtype, k.get_device()
+    if k.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2 or dt not in _CODES or (q is None) != (q_out is None):
+        raise T5Error(-8, "want float32 or bfloat16 k [tokens, kv_heads, d_kv], pools [n_pages, page_size, kv_heads, d_kv], a "
+                          "2-D page table, and q with q_out")
+    shape, ps, table = k.shape, k_pages.shape, page_table.shape
+    n, g, d = shape
+    ldk, ldv, st = _row_stride(k, shape, d), _row_stride(v, shape, d) if v.shape == shape else -1, page_table.stride()
+    pool = _pool_strides(k_pages, v_pages, ps) if v_pages.shape == ps else None
     h = ldq = ldqo = qp = qop = 0
+    fine = True
     if q is not None:
-        _require(q.dim() == 3 and q_out is not None, "q: want [tokens, heads, d_kv] and q_out")
-        h = q.shape[1]
-        ldq, ldqo = _heads(q, "q", (n, h, d), k.dtype, device), _heads(q_out, "q_out", (n, h, d), k.dtype, device)
-        qp, qop = q.data_ptr(), q_out.data_ptr()
-    _check(lib().t5_paged_kv_append(code, n, h, g, d, qp, ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, qop, ldqo,
-                                    seq_of_token.data_ptr(), positions.data_ptr(), rot_dim, rot_base,
-                                    int(rot_interleaved), *pool, page_table.shape[0], max_pages, ld_table, stream))
+        qs = q.shape
+        fine = len(qs) == 3 and qs[0] == n and qs[2] == d and q_out.shape == qs and q.dtype is dt and q_out.dtype is dt and \
+            q.get_device() == dev and q_out.get_device() == dev
+        if fine:
+            h, ldq, ldqo, qp, qop = qs[1], _row_stride(q, qs, d), _row_stride(q_out, qs, d), q.data_ptr(), q_out.data_ptr()
+    if not (fine and ldk >= 0 and ldv >= 0 and ldq >= 0 and ldqo >= 0 and pool and ps[2] == g and ps[3] == d and v.dtype is dt
+            and k_pages.dtype is dt and v_pages.dtype is dt and page_table.dtype is _I32 and seq_of_token.dtype is _I32
+            and positions.dtype is _I32 and seq_of_token.numel() == n and positions.numel() == n and st[1] == 1
+            and seq_of_token.is_contiguous() and positions.is_contiguous()
+            and dev == v.get_device() == k_pages.get_device() == v_pages.get_device() == page_table.get_device()
+            == seq_of_token.get_device() == positions.get_device() == torch.cuda.current_device()):
+        heads = None if q is None else (n, q.shape[1], d)
+        _refuse(torch.cuda.current_device(), [
+            ("k", k, dt, shape), ("v", v, dt, shape), ("k_pages", k_pages, dt, (ps[0], ps[1], g, d)),
+            ("v_pages", v_pages, dt, ps), ("page_table", page_table, _I32, table), ("seq_of_token", seq_of_token, _I32, (n,)),
+            ("positions", positions, _I32, (n,))] + ([] if q is None else [("q", q, dt, heads), ("q_out", q_out, dt, heads)]))
+    rc = lib().t5_paged_kv_append(_CODES[dt], n, h, g, d, qp, ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, qop, ldqo,
+                                  seq_of_token.data_ptr(), positions.data_ptr(), rot_dim, rot_base, int(rot_interleaved),
+                                  k_pages.data_ptr(), v_pages.data_ptr(), ps[0], ps[1], *pool, page_table.data_ptr(), table[0],
+                                  table[1], st[0] if table[0] > 1 else table[1], _raw_stream(dev))
+    if rc:
+        _check(rc)
 
 
 def t5_paged_attention_workspace_bytes(n_rows, n_q, n_heads, n_kv_heads, d_kv):
@@ -462,57 +471,77 @@ def t5_paged_attention_workspace_bytes(n_rows, n_q, n_heads, n_kv_heads, d_kv):
 def t5_paged_attention(q, k_pages, v_pages, page_table, lens, out, workspace, scale=1.0, n_q=1, bias=None, lse=None):
     """q, out [rows, heads, d_kv]; lens [rows]; n_q rows per row of the page table; bias [heads, n_bias] float32, the
     near end last; lse [rows, heads] float32; see the header."""
-    device, stream = _place(q)
-    code = _dtype_code(q)
-    _require(q.dim() == 3 and k_pages.dim() == 4 and k_pages.dtype == q.dtype, "q: want [rows, heads, d_kv] of the pools' type")
-    r, h, d = q.shape
-    g = k_pages.shape[2]
-    _require(k_pages.shape[3] == d and n_q >= 1 and page_table.dim() == 2 and page_table.shape[0] * n_q == r,
-             "want the pools' d_kv and n_q rows of q per row of the page table")
-    pool, max_pages, ld_table = _pool(k_pages, v_pages, page_table, device)
-    ldq, ldo = _heads(q, "q", (r, h, d), q.dtype, device), _heads(out, "out", (r, h, d), q.dtype, device)
-    _dense(lens, "lens", (r,), torch.int32, device)
+    dt, dev = q.dtype, q.get_device()
+    if q.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2 or dt not in _CODES or (bias is not None and bias.dim() != 2):
+        raise T5Error(-8, "want float32 or bfloat16 q [rows, heads, d_kv], pools [n_pages, page_size, kv_heads, d_kv], a 2-D "
+                          "page table, a 2-D bias")
+    shape, ps, table = q.shape, k_pages.shape, page_table.shape
+    r, h, d = shape
+    g = ps[2]
+    ldq, ldo, st = _row_stride(q, shape, d), _row_stride(out, shape, d) if out.shape == shape else -1, page_table.stride()
+    pool = _pool_strides(k_pages, v_pages, ps) if v_pages.shape == ps else None
     n_bias = bp = lp = 0
+    fine = True
     if bias is not None:
-        n_bias = bias.shape[-1]
-        _dense(bias, "bias", (h, n_bias), torch.float32, device)
-        _require(bias.is_contiguous(), "bias: want a contiguous tensor")
-        bp = bias.data_ptr()
+        n_bias, bp = bias.shape[1], bias.data_ptr()
+        fine = bias.shape[0] == h and bias.dtype is _F32 and bias.is_contiguous() and bias.get_device() == dev
     if lse is not None:
-        _dense(lse, "lse", (r, h), torch.float32, device)
-        _require(lse.is_contiguous(), "lse: want a contiguous tensor")
         lp = lse.data_ptr()
-    _require(workspace.device == device and workspace.is_contiguous(), "workspace: want a contiguous tensor on the device")
-    _check(lib().t5_paged_attention(code, r, n_q, h, g, d, scale, q.data_ptr(), ldq, *pool, max_pages, ld_table,
-                                    lens.data_ptr(), bp, n_bias, out.data_ptr(), ldo, lp, workspace.data_ptr(),
-                                    workspace.numel() * workspace.element_size(), stream))
+        fine = fine and lse.shape == shape[:2] and lse.dtype is _F32 and lse.is_contiguous() and lse.get_device() == dev
+    if not (fine and ldq >= 0 and ldo >= 0 and pool and ps[3] == d and table[0] * n_q == r and st[1] == 1 and out.dtype is dt
+            and k_pages.dtype is dt and v_pages.dtype is dt and page_table.dtype is _I32 and lens.dtype is _I32
+            and lens.numel() == r and lens.is_contiguous() and workspace.is_contiguous()
+            and dev == out.get_device() == k_pages.get_device() == v_pages.get_device() == page_table.get_device()
+            == lens.get_device() == workspace.get_device() == torch.cuda.current_device()):
+        _refuse(torch.cuda.current_device(), [
+            ("q", q, dt, shape), ("out", out, dt, shape), ("k_pages", k_pages, dt, (ps[0], ps[1], g, d)),
+            ("v_pages", v_pages, dt, ps), ("page_table (n_q rows of q per row)", page_table, _I32, (r // max(n_q, 1), table[1])),
+            ("lens", lens, _I32, (r,)), ("workspace", workspace, workspace.dtype, workspace.shape)]
+            + ([] if bias is None else [("bias", bias, _F32, (h, n_bias))]) + ([] if lse is None else [("lse", lse, _F32, (r, h))]))
+    rc = lib().t5_paged_attention(_CODES[dt], r, n_q, h, g, d, scale, q.data_ptr(), ldq, k_pages.data_ptr(),
+                                  v_pages.data_ptr(), ps[0], ps[1], *pool, page_table.data_ptr(), table[1],
+                                  st[0] if table[0] > 1 else table[1], lens.data_ptr(), bp, n_bias, out.data_ptr(), ldo, lp,
+                                  workspace.data_ptr(), workspace.nbytes, _raw_stream(dev))
+    if rc:
+        _check(rc)
 
 
 def t5_verify_draft(target, draft, draft_tokens, n_draft, u_accept, u_sample, out_tokens, n_accepted):
     """target [seqs, drafts + 1, vocab], draft [seqs, drafts, vocab] or None, draft_tokens / u_accept [seqs, drafts],
     n_draft [seqs] or None, u_sample [seqs] -> out_tokens [seqs, drafts + 1], n_accepted [seqs]; see the header."""
-    device, stream = _place(target)
-    code = _dtype_code(target)
-    _require(target.dim() == 3 and target.shape[1] >= 1, "target: want [seqs, drafts + 1, vocab]")
+    dt, dev = target.dtype, target.get_device()
+    if target.dim() != 3 or target.shape[1] < 1 or dt not in _CODES:
+        raise T5Error(-8, "target: want float32 or bfloat16 [seqs, drafts + 1, vocab]")
     s, k1, v = target.shape
     k = k1 - 1
-
-    def strides(t, name, shape):
-        _dense(t, name, shape, target.dtype, device)
-        return (t.data_ptr(), t.stride(0) if shape[0] > 1 else 0, t.stride(1) if shape[1] > 1 else v)
-
-    def rows(t, name, dtype, width):
-        _dense(t, name, (s, width), dtype, device)
-        return t.data_ptr(), t.stride(0) if s > 1 else width
-    tgt = strides(target, "target", (s, k1, v))
-    drf = (0, 0, v) if draft is None or k == 0 else strides(draft, "draft", (s, k, v))
-    xs, us = rows(draft_tokens, "draft_tokens", torch.int32, k), rows(u_accept, "u_accept", torch.float32, k)
-    out = rows(out_tokens, "out_tokens", torch.int32, k1)
-    for t, name, dt in ((u_sample, "u_sample", torch.float32), (n_accepted, "n_accepted", torch.int32)):
-        _dense(t, name, (s,), dt, device)
-    np_ = 0
+    tt, tx, tu, to = target.stride(), draft_tokens.stride(), u_accept.stride(), out_tokens.stride()
+    np_ = dp = ds = 0
+    dr = v
+    fine = True
     if n_draft is not None:
-        _dense(n_draft, "n_draft", (s,), torch.int32, device)
         np_ = n_draft.data_ptr()
-    _check(lib().t5_verify_draft(code, s, k, v, *tgt, *drf, *xs, np_, *us, u_sample.data_ptr(), *out,
-                                 n_accepted.data_ptr(), stream))
+        fine = n_draft.dtype is _I32 and n_draft.numel() == s and n_draft.is_contiguous() and n_draft.get_device() == dev
+    if draft is not None and k > 0:
+        td, dp = draft.stride(), draft.data_ptr()
+        fine = fine and draft.dtype is dt and draft.shape == (s, k, v) and (td[2] == 1 or v == 1) and draft.get_device() == dev
+        if fine:
+            ds, dr = td[0] if s > 1 else 0, td[1] if k > 1 else v
+    if not (fine and (tt[2] == 1 or v == 1) and draft_tokens.shape == (s, k) and u_accept.shape == (s, k)
+            and out_tokens.shape == (s, k1) and (k <= 1 or (tx[1] == 1 and tu[1] == 1)) and (k == 0 or to[1] == 1)
+            and draft_tokens.dtype is _I32 and u_accept.dtype is _F32 and u_sample.dtype is _F32 and out_tokens.dtype is _I32
+            and n_accepted.dtype is _I32 and u_sample.numel() == s and n_accepted.numel() == s and u_sample.is_contiguous()
+            and n_accepted.is_contiguous()
+            and dev == draft_tokens.get_device() == u_accept.get_device() == u_sample.get_device() == out_tokens.get_device()
+            == n_accepted.get_device() == torch.cuda.current_device()):
+        _refuse(torch.cuda.current_device(), [
+            ("target", target, dt, (s, k1, v)), ("draft_tokens", draft_tokens, _I32, (s, k)), ("u_accept", u_accept, _F32, (s, k)),
+            ("u_sample", u_sample, _F32, (s,)), ("out_tokens", out_tokens, _I32, (s, k1)), ("n_accepted", n_accepted, _I32, (s,))]
+            + ([] if draft is None else [("draft", draft, dt, (s, k, v))])
+            + ([] if n_draft is None else [("n_draft", n_draft, _I32, (s,))]))
+    one = s <= 1
+    rc = lib().t5_verify_draft(_CODES[dt], s, k, v, target.data_ptr(), 0 if one else tt[0], tt[1] if k else v, dp, ds, dr,
+                               draft_tokens.data_ptr(), k if one else tx[0], np_, u_accept.data_ptr(), k if one else tu[0],
+                               u_sample.data_ptr(), out_tokens.data_ptr(), k1 if one else to[0], n_accepted.data_ptr(),
+                               _raw_stream(dev))
+    if rc:
+        _check(rc)

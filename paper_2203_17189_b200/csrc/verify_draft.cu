@@ -6,8 +6,11 @@
 // max(target_a - draft_a, 0) when x_a was refused, from target_n when none was.  The tokens then follow the target's
 // distribution.  The draw inverts the cumulative sum: the first v with sum_{i <= v} r_i > u sum_i r_i.
 //
-// All arithmetic on the probabilities is float64 (a product of two float32 values and a difference are exact there, a sum
-// of 10^5 of them is off by 10^-16 of the total), so the outcome does not depend on the order of the sums.
+// A float32 sum of 10^5 probabilities is off by enough to move the drawn point over a border, so sums carry about 48 bits:
+// u draft < target is decided in float64, where the product of two float32 values is exact; differences and the sums of a
+// lane are kept as two float32 parts (error-free transformations: the rounding error of a + b is itself a float32 and
+// is added up beside the sum); everything behind that is float64.  (Float64 from the start cost 19.2 instead of 11.6 us on
+// 256 bfloat16 rows of 32128: conversions and float64 comparisons of every value.)
 //
 // Bound: latency.  Only the row behind the last accepted token is read, once: 2 V values per sequence.  A cluster of CTAs
 // takes one sequence; every warp sums runs of the row, the CTAs exchange their totals through distributed shared memory,
@@ -24,7 +27,7 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kMaxRuns = 1024;      // runs of one CTA; a run = 32 lanes x 16 bytes of the row
+constexpr int kMaxRuns = 2048;      // runs of one CTA; a run = LN values of each of a warp's lanes
 
 struct VerifyParams {
   const void *target, *draft;
@@ -36,8 +39,29 @@ struct VerifyParams {
   int K, V, vec;
 };
 
-// entry of a distribution; what is not a positive finite number has no mass
-__device__ __forceinline__ double mass(double r) { return r > 0.0 && r < INFINITY ? r : 0.0; }
+// a sum in two parts: hi the rounded sum, lo what the roundings lost
+struct Sum2 {
+  float hi = 0.f, lo = 0.f;
+  __device__ __forceinline__ void add(float x, float x_lo) {
+    const float t = hi + x, b = t - hi;
+    lo += ((hi - (t - b)) + (x - b)) + x_lo;
+    hi = t;
+  }
+  __device__ __forceinline__ double value() const { return (double)hi + (double)lo; }
+};
+// max(p - q, 0) in two parts; what is not a positive finite number has no mass
+template <bool DIFF>
+__device__ __forceinline__ void mass(float p, float q, float& hi, float& lo) {
+  float h = p, l = 0.f;
+  if (DIFF) {
+    h = p - q;
+    const float b = h - p;
+    l = (p - (h - b)) - (q + b);
+  }
+  const bool some = __float_as_uint(h) - 1u < 0x7f7fffffu;      // 0 < h < infinity
+  hi = some ? h : 0.f;
+  lo = DIFF && some ? l : 0.f;
+}
 
 // N consecutive values from element v (those at or behind V: 0)
 template <typename T, int N>
@@ -53,10 +77,56 @@ __device__ __forceinline__ void load_run(const T* p, int v, int V, bool vec, flo
   }
 }
 
-template <typename T>
+// What the lanes of a warp hold of a run: chunk c of a lane = elements run * 32 LN + c * 32 N + lane * N ... of the row
+template <typename T, int LN> struct RunOf {
+  static constexpr int N = 16 / sizeof(T), NC = LN / N, SIZE = 32 * LN;
+  float hi[LN], lo[LN];
+  template <bool DIFF>
+  __device__ __forceinline__ void load(const T* p, const T* q, int run, int V, bool vec, int hole, int lane) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int v = run * SIZE + c * 32 * N + lane * N;
+      float pf[N], qf[N];
+      load_run<T, N>(p, v, V, vec, pf);
+      if (DIFF) load_run<T, N>(q, v, V, vec, qf);
+      if (hole >= v && hole < v + N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) pf[i] = v + i == hole ? 0.f : pf[i];
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) mass<DIFF>(pf[i], DIFF ? qf[i] : 0.f, hi[c * N + i], lo[c * N + i]);
+    }
+  }
+  __device__ __forceinline__ void get(const T* p, const T* q, int run, int V, bool vec, int hole, int lane) {
+    if (q != nullptr) load<true>(p, q, run, V, vec, hole, lane);
+    else load<false>(p, q, run, V, vec, hole, lane);
+  }
+};
+
+// Sums of this warp's runs (run w, w + kWarps, ... of [0, n)) into shared memory
+template <typename T, int LN, bool DIFF>
+__device__ __forceinline__ void sum_runs(const T* p, const T* q, int r0, int n, int V, bool vec, int hole, double* runs) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 2
+  for (int run = threadIdx.x >> 5; run < n; run += kWarps) {
+    RunOf<T, LN> r;
+    r.template load<DIFF>(p, q, r0 + run, V, vec, hole, lane);
+    Sum2 even, odd;      // two chains of dependent additions instead of one
+#pragma unroll
+    for (int i = 0; i < LN; i += 2) { even.add(r.hi[i], r.lo[i]); odd.add(r.hi[i + 1], r.lo[i + 1]); }
+    even.add(odd.hi, odd.lo);
+    double sum = even.value();
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) runs[run] = sum;
+  }
+}
+
+template <typename T, int LN>
 __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant__ VerifyParams a) {
   pdl_sync();
-  constexpr int N = 16 / sizeof(T), RUN = 32 * N;
+  using R = RunOf<T, LN>;
+  constexpr int N = R::N, NC = R::NC;
   cg::cluster_group cluster = cg::this_cluster();
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int s = blockIdx.x / cs, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
@@ -66,54 +136,39 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
   __shared__ int first, run_at;
   const int K = a.K, V = a.V;
   const int n = a.n_draft != nullptr ? min(max(a.n_draft[s], 0), K) : K;
-  if (tid == 0) { first = n; run_at = -1; }
+  const double u = a.u_sample[s];
+  if (tid == 0) { first = K; run_at = -1; }
   __syncthreads();
   const T* tgt = reinterpret_cast<const T*>(a.target) + s * a.t_seq;
   const T* drf = a.draft != nullptr ? reinterpret_cast<const T*>(a.draft) + s * a.d_seq : nullptr;
   const int* xs = a.x + s * a.ld_x;
-  for (int i = tid; i < n; i += kThreads) {
+  for (int i = tid; i < K; i += kThreads) {      // all K, so that no load waits for n
     const int x = xs[i];
+    const float ui = a.u[s * a.ld_u + i];
     bool ok = false;
     if (x >= 0 && x < V) {
       const double p = to_f(tgt[i * a.t_row + x]), q = drf != nullptr ? to_f(drf[i * a.d_row + x]) : 1.0;
-      ok = (double)a.u[s * a.ld_u + i] * q < p;
+      ok = (double)ui * q < p;
     }
     if (!ok) atomicMin(&first, i);
   }
   __syncthreads();
-  const int acc = first;
+  const int acc = min(first, n);
   const bool refused = acc < n;
   const T* tr = tgt + acc * a.t_row;
   const T* dr = refused && drf != nullptr ? drf + acc * a.d_row : nullptr;
   const int hole = refused && drf == nullptr ? xs[acc] : -1;
-  const double u = a.u_sample[s];
 
-  // this CTA's runs: [r0, r1) of ceil(V / RUN)
-  const int all = (V + RUN - 1) / RUN;
+  // this CTA's runs: [r0, r1) of those of the row
+  const int all = (V + R::SIZE - 1) / R::SIZE;
   const int r0 = (int)((int64_t)all * rank / cs), r1 = (int)((int64_t)all * (rank + 1) / cs);
   int token = -1;
   // second attempt: the refused draft equals the target everywhere it has mass, nothing is left; draw from the target
   for (int attempt = 0; attempt < 2; ++attempt) {
     const T* d = attempt == 0 ? dr : nullptr;
     const int skip = attempt == 0 ? hole : -1;
-    auto values = [&](int run, double (&r)[N]) {
-      const int v = run * RUN + lane * N;
-      float p[N], q[N];
-      load_run<T, N>(tr, v, V, a.vec, p);
-      if (d != nullptr) load_run<T, N>(d, v, V, a.vec, q);
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        r[i] = v + i == skip ? 0.0 : mass(d != nullptr ? (double)p[i] - (double)q[i] : (double)p[i]);
-    };
-    for (int run = r0 + w; run < r1; run += kWarps) {
-      double r[N], sum = 0.0;
-      values(run, r);
-#pragma unroll
-      for (int i = 0; i < N; ++i) sum += r[i];
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if (lane == 0) runs[run - r0] = sum;
-    }
+    if (d != nullptr) sum_runs<T, LN, true>(tr, d, r0, r1 - r0, V, a.vec, skip, runs);
+    else sum_runs<T, LN, false>(tr, d, r0, r1 - r0, V, a.vec, skip, runs);
     __syncthreads();
     // inclusive prefix sums of the runs
     if (w == 0) {
@@ -164,31 +219,41 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
     }
     __syncthreads();
     if (w != 0) return;
-    double r[N], sum = 0.0;
-    values(r0 + run_at, r);
+    R r;
+    r.get(tr, d, r0 + run_at, V, a.vec, skip, lane);
+    double reached = run_before;      // in front of the chunk
+    int some = -1;                    // this lane's last value with mass, should rounding leave none beyond t
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum += r[i];
-    double inc = sum;
+    for (int c = 0; c < NC; ++c) {
+      double sum = 0.0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const double y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
-    }
-    // lane's candidates: the first of its values that reaches beyond t; the last one with mass
-    double run_sum = run_before + inc - sum;
-    int hit = -1, some = -1;
+      for (int i = 0; i < N; ++i) sum += (double)r.hi[c * N + i] + (double)r.lo[c * N + i];
+      double inc = sum;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      run_sum += r[i];
-      const int v = (r0 + run_at) * RUN + lane * N + i;
-      if (r[i] > 0.0) {
-        if (hit < 0 && run_sum > t) hit = v;
-        some = v;
+      for (int o = 1; o < 32; o <<= 1) {
+        const double y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
       }
+      double at = reached + inc - sum;
+      int hit = -1;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        at += (double)r.hi[c * N + i] + (double)r.lo[c * N + i];
+        const int v = (r0 + run_at) * R::SIZE + c * 32 * N + lane * N + i;
+        if (r.hi[c * N + i] > 0.f) {
+          if (hit < 0 && at > t) hit = v;
+          some = v;
+        }
+      }
+      const uint32_t hits = __ballot_sync(0xffffffffu, hit >= 0);
+      if (hits && token < 0) token = __shfl_sync(0xffffffffu, hit, __ffs(hits) - 1);
+      reached += __shfl_sync(0xffffffffu, inc, 31);
     }
-    const uint32_t hits = __ballot_sync(0xffffffffu, hit >= 0), somes = __ballot_sync(0xffffffffu, some >= 0);
-    if (hits) token = __shfl_sync(0xffffffffu, hit, __ffs(hits) - 1);
-    else if (somes) token = __shfl_sync(0xffffffffu, some, 31 - __clz(somes));
+    if (token < 0) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) some = max(some, __shfl_xor_sync(0xffffffffu, some, o));
+      token = some;
+    }
     break;
   }
   // the owner's first warp, or (nothing to draw from) the first CTA
@@ -198,7 +263,18 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
   if (lane == 0) a.accepted[s] = acc;
 }
 
-template <typename T>
+// CTAs per sequence: as many as leave every SM at most two.  Measured (vocabulary 32128, float32 with draft
+// probabilities, us with 8 / 4 / 2 / 1 CTAs): 1 sequence 5.4 / 6.1 / 7.7 / 10.8, 32: 6.7 / 6.9 / 8.0 / 11.1,
+// 64: 12.1 / 7.5 / 8.0 / 11.1, 148: 25.1 / 16.9 / 10.9 / 12.2, 256: 47.1 / 29.2 / 21.9 / 18.2.
+template <int LN>
+int cluster_size(int n_seqs, int vocab) {
+  int cs = 8;
+  while (cs > 1 && n_seqs * cs > 2 * 148) cs /= 2;
+  while (cs < 8 && vocab > cs * kMaxRuns * 32 * LN) cs *= 2;      // a CTA's table of runs
+  return cs;
+}
+
+template <typename T, int LN>
 cudaError_t run(const VerifyParams& a, int S, int cs, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(S * cs)); cfg.blockDim = dim3(kThreads); cfg.stream = st;
@@ -208,7 +284,7 @@ cudaError_t run(const VerifyParams& a, int S, int cs, cudaStream_t st) {
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, verify_kernel<T>, a);
+  return cudaLaunchKernelEx(&cfg, verify_kernel<T, LN>, a);
 }
 
 }  // namespace
@@ -243,9 +319,9 @@ extern "C" int t5_verify_draft(int32_t dtype, int32_t n_seqs, int32_t max_draft,
   };
   if (((uintptr_t)d_target % es) || ((uintptr_t)a.draft % es)) return T5_ERR_ALIGN;
   a.vec = even(d_target, a.t_seq, a.t_row) && (a.draft == nullptr || even(a.draft, a.d_seq, a.d_row));
-  // eight CTAs per sequence, which the largest vocabulary also needs for its table of runs; with many sequences fewer
-  const int cs = 8;
-  const cudaError_t e = dtype == DT_F32 ? run<float>(a, n_seqs, cs, (cudaStream_t)stream)
-                                        : run<bf16>(a, n_seqs, cs, (cudaStream_t)stream);
+  constexpr int LN = 8;      // 16 and 32 values per lane: 14.3 and 15.9 instead of 12.2 us on 148 float32 sequences
+  const int cs = cluster_size<LN>(n_seqs, vocab);
+  const cudaError_t e = dtype == DT_F32 ? run<float, LN>(a, n_seqs, cs, (cudaStream_t)stream)
+                                        : run<bf16, LN>(a, n_seqs, cs, (cudaStream_t)stream);
   return e == cudaSuccess ? T5_OK : T5_ERR_CUDA;
 }
