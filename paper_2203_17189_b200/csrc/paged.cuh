@@ -16,7 +16,7 @@ __device__ __forceinline__ void paged_report(int* status, int code) {
 struct FastDiv {
   uint32_t d, m, s;
   FastDiv() = default;
-  __host__ explicit FastDiv(uint32_t dd) : d(dd), m(0), s(0) {
+  __host__ explicit FastDiv(uint32_t dd) : d(dd), m(0), s(0) {      // 0: never divided by
     while ((1ull << s) < d) ++s;
     if (s > 0) m = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
   }

@@ -17,6 +17,7 @@
 namespace {
 
 constexpr int kMaxPairs = 64;      // rot_dim <= d_kv <= 128
+constexpr int kAppendThreads = 256, kMaxTok = 8;
 
 struct AppendParams {
   const char *k, *v;
@@ -27,7 +28,11 @@ struct AppendParams {
   int tokens_per_seq, n_tokens, n_seqs;
   int H, G, d_bytes;                // q heads (0: no q), kv heads, bytes of one head
   int rot_bytes, interleaved;       // bytes of one head that are rotated
-  int parts;                        // warps that share one token
+  int tok;                          // tokens of a CTA
+  FastDiv rot_units, per_rot;       // pairs of 16-byte chunks rotated in a head; in a token's q and k heads
+  FastDiv rest, per_rest;           // chunks only copied, in a head; in a token's q and k heads
+  int v_shift;                      // log2 of the chunks of a head
+  FastDiv per_v;                    // chunks of a token's v
   PagedPool pool;
   int* status;
   double turns[kMaxPairs];          // base^(-2 i / rot_dim) / 2 pi
@@ -65,100 +70,131 @@ template <> struct Chunk<bf16> {
   }
 };
 
-// One warp: `parts` warps share a token's heads.  Lane = (head, unit): a unit is the two 16-byte chunks that hold N
-// pairs, the same unit in every head the lane visits, so its sines and cosines are computed once per token.
-template <typename T>
-__global__ void __launch_bounds__(256) paged_append_kernel(const __grid_constant__ AppendParams a) {
+// Calls from(u) -> source, then to(u, loaded) for the CTA's share of [0, n): BATCH loads per thread are on their way
+// before the first store.  gridDim.y CTAs share the items of a group of tokens.
+template <int BATCH, int CHUNKS, typename From, typename To>
+__device__ __forceinline__ void each_item(int n, From from, To to) {
+  const int end = (int)((int64_t)n * (blockIdx.y + 1) / gridDim.y);
+  for (int u = (int)((int64_t)n * blockIdx.y / gridDim.y) + threadIdx.x; u < end; u += kAppendThreads * BATCH) {
+    uint4 x[BATCH][CHUNKS];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b)
+      if (u + b * kAppendThreads < end) from(u + b * kAppendThreads, x[b]);
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b)
+      if (u + b * kAppendThreads < end) to(u + b * kAppendThreads, x[b]);
+  }
+}
+
+// A CTA takes `tok` tokens: first where they go and the sines and cosines of their pairs, into shared memory, then all
+// their chunks, thread by thread.  (A warp per token, with the angles in its registers, held too few loads in flight:
+// 122 us on 16 prompts of up to 2048 tokens, 48 heads of 128 columns.)
+template <typename T, int INTERLEAVED>
+__global__ void __launch_bounds__(kAppendThreads, 5) paged_append_kernel(const __grid_constant__ AppendParams a) {
   pdl_sync();
-  constexpr int N = Chunk<T>::N;
-  const int lane = threadIdx.x & 31;
-  const int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int t = (int)(task / a.parts), part = (int)(task % a.parts);
-  if (t >= a.n_tokens) return;
-  const int pos = a.pos[t];
-  const int s = a.seq != nullptr ? a.seq[t] : t / a.tokens_per_seq;
-  char *kd = nullptr, *vd = nullptr;      // NULL: padding or a bad place, nothing is written
-  if (pos >= 0) {
-    const int pi = (int)a.pool.ps.div((uint32_t)pos);
-    int page = -1;
-    if (s >= 0 && s < a.n_seqs && pi < a.pool.max_pages) page = a.pool.table[s * a.pool.ld_table + pi];
-    if (page >= 0 && page < a.pool.n_pages) {
-      const int64_t off = page * a.pool.page_stride + (pos - pi * a.pool.page_size) * a.pool.slot_stride;
-      kd = a.pool.k + off;
-      vd = a.pool.v + off;
-    } else if (lane == 0) {
-      paged_report(a.status, PAGED_BAD_APPEND);
+  constexpr int N = Chunk<T>::N, BATCH = 2;
+  __shared__ float2 sc[kMaxTok][kMaxPairs];
+  __shared__ int64_t place[kMaxTok];      // byte offset in the pools; -1: a bad place, -2: padding
+  const int tid = threadIdx.x;
+  const int64_t t0 = (int64_t)blockIdx.x * a.tok;
+  const int nt = (int)min((int64_t)a.tok, a.n_tokens - t0);
+  if (tid < nt) {
+    const int pos = a.pos[t0 + tid];
+    const int s = a.seq != nullptr ? a.seq[t0 + tid] : (int)((t0 + tid) / a.tokens_per_seq);
+    int64_t at = -2;
+    if (pos >= 0) {
+      const int pi = (int)a.pool.ps.div((uint32_t)pos);
+      int page = -1;
+      if (s >= 0 && s < a.n_seqs && pi < a.pool.max_pages) page = a.pool.table[s * a.pool.ld_table + pi];
+      at = -1;
+      if (page >= 0 && page < a.pool.n_pages)
+        at = page * a.pool.page_stride + (pos - pi * a.pool.page_size) * a.pool.slot_stride;
+      else if (blockIdx.y == 0)
+        paged_report(a.status, PAGED_BAD_APPEND);
+    }
+    place[tid] = at;
+  }
+  const int pairs = (int)a.rot_units.d * N;
+  for (int i = tid; i < nt * kMaxPairs; i += kAppendThreads) {
+    const int t = i / kMaxPairs, pair = i % kMaxPairs;
+    if (a.rot_bytes > 0 && pair < pairs) {
+      const double turn = (double)max(a.pos[t0 + t], 0) * a.turns[pair];
+      sincospif(2.f * (float)(turn - rint(turn)), &sc[t][pair].x, &sc[t][pair].y);
     }
   }
-  const char* ks = a.k + t * a.ldk;
-  const char* vs = a.v + t * a.ldv;
-  const char* qs = a.q + t * a.ldq;
-  char* qd = a.q_out + t * a.ldqo;
-  const int H = a.H, G = a.G, db = a.d_bytes;
-  // rotated columns of the q and k heads [0, H + G)
+  __syncthreads();
+  const int H = a.H;
+  // source and destination of column byte o of head h (q heads first) of the CTA's token t; NULL: none
+  auto src = [&](int t, int h, int o) -> const char* {
+    if (h < H) return a.q + (t0 + t) * a.ldq + h * a.d_bytes + o;
+    return place[t] == -2 ? nullptr : a.k + (t0 + t) * a.ldk + (h - H) * a.d_bytes + o;
+  };
+  auto dst = [&](int t, int h, int o) -> char* {
+    if (h < H) return a.q_out + (t0 + t) * a.ldqo + h * a.d_bytes + o;
+    return place[t] < 0 ? nullptr : a.pool.k + place[t] + (h - H) * a.pool.head_stride + o;
+  };
+  const int second = INTERLEAVED ? 16 : a.rot_bytes / 2;      // from a unit's first chunk to its second
   if (a.rot_bytes > 0) {
-    const int units = a.rot_bytes / 32, hstep = 32 / units;
-    const int c = lane % units, h_lane = lane / units;
-    const int o0 = a.interleaved ? c * 32 : c * 16, o1 = a.interleaved ? o0 + 16 : o0 + a.rot_bytes / 2;
-    float cs[N], sn[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const double turn = (double)(pos > 0 ? pos : 0) * a.turns[c * N + i];
-      sincospif(2.f * (float)(turn - rint(turn)), &sn[i], &cs[i]);
-    }
-    const int h0 = (int)((int64_t)(H + G) * part / a.parts), h1 = (int)((int64_t)(H + G) * (part + 1) / a.parts);
-    if (h_lane < hstep) {
-#pragma unroll 4
-      for (int h = h0 + h_lane; h < h1; h += hstep) {
-        const bool is_q = h < H;
-        const char* src = is_q ? qs + (int64_t)h * db : ks + (int64_t)(h - H) * db;
-        char* dst = is_q ? qd + (int64_t)h * db : kd + (h - H) * a.pool.head_stride;
-        if (!is_q && kd == nullptr) continue;
-        float x0[N], x1[N], y0[N], y1[N];
-        Chunk<T>::get(*reinterpret_cast<const uint4*>(src + o0), x0);
-        Chunk<T>::get(*reinterpret_cast<const uint4*>(src + o1), x1);
-        if (a.interleaved) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {      // the two chunks are one run of 2 N columns: pair i = entries 2 i, 2 i + 1
-            const float e = 2 * i < N ? x0[(2 * i) % N] : x1[(2 * i) % N], o = 2 * i < N ? x0[(2 * i + 1) % N] : x1[(2 * i + 1) % N];
-            const float u = e * cs[i] - o * sn[i], w = o * cs[i] + e * sn[i];
-            if (2 * i < N) { y0[(2 * i) % N] = u; y0[(2 * i + 1) % N] = w; } else { y1[(2 * i) % N] = u; y1[(2 * i + 1) % N] = w; }
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            y0[i] = x0[i] * cs[i] - x1[i] * sn[i];
-            y1[i] = x1[i] * cs[i] + x0[i] * sn[i];
-          }
-        }
-        *reinterpret_cast<uint4*>(dst + o0) = Chunk<T>::put(y0);
-        *reinterpret_cast<uint4*>(dst + o1) = Chunk<T>::put(y1);
+    struct Unit { int t, h, c; };
+    auto unit = [&](int u) {
+      Unit x;
+      x.t = (int)a.per_rot.div(u);
+      const int r = u - x.t * (int)a.per_rot.d;
+      x.h = (int)a.rot_units.div(r);
+      x.c = r - x.h * (int)a.rot_units.d;
+      return x;
+    };
+    each_item<BATCH, 2>(nt * (int)a.per_rot.d, [&](int u, uint4 (&x)[2]) {
+      const Unit i = unit(u);
+      const char* p = src(i.t, i.h, i.c * (INTERLEAVED ? 32 : 16));
+      if (p != nullptr) {
+        x[0] = *reinterpret_cast<const uint4*>(p);
+        x[1] = *reinterpret_cast<const uint4*>(p + second);
       }
-    }
+    }, [&](int u, const uint4 (&x)[2]) {
+      const Unit i = unit(u);
+      char* p = dst(i.t, i.h, i.c * (INTERLEAVED ? 32 : 16));
+      if (p == nullptr) return;
+      float f[2 * N], y[2 * N];
+      Chunk<T>::get(x[0], f);
+      Chunk<T>::get(x[1], f + N);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {      // pair e of the unit: entries e and e + N, or 2 e and 2 e + 1
+        const int lo = INTERLEAVED ? 2 * e : e, hi = INTERLEAVED ? 2 * e + 1 : e + N;
+        const float2 t = sc[i.t][i.c * N + e];
+        y[lo] = f[lo] * t.y - f[hi] * t.x;
+        y[hi] = f[hi] * t.y + f[lo] * t.x;
+      }
+      *reinterpret_cast<uint4*>(p) = Chunk<T>::put(y);
+      *reinterpret_cast<uint4*>(p + second) = Chunk<T>::put(y + N);
+    });
   }
   // columns that are only copied: the rest of the q and k heads, and all of v
-  const int rest = (db - a.rot_bytes) / 16;
-  if (rest > 0) {
-    const int n = (H + G) * rest;
-    const int u1 = (int)((int64_t)n * (part + 1) / a.parts);
-#pragma unroll 4
-    for (int u = (int)((int64_t)n * part / a.parts) + lane; u < u1; u += 32) {
-      const int h = u / rest, o = a.rot_bytes + (u - h * rest) * 16;
-      if (h < H) *reinterpret_cast<uint4*>(qd + (int64_t)h * db + o) = *reinterpret_cast<const uint4*>(qs + (int64_t)h * db + o);
-      else if (kd != nullptr)
-        *reinterpret_cast<uint4*>(kd + (h - H) * a.pool.head_stride + o) =
-            *reinterpret_cast<const uint4*>(ks + (int64_t)(h - H) * db + o);
-    }
+  if (a.rest.d > 0) {
+    each_item<2 * BATCH, 1>(nt * (int)a.per_rest.d, [&](int u, uint4 (&x)[1]) {
+      const int t = (int)a.per_rest.div(u), r = u - t * (int)a.per_rest.d, h = (int)a.rest.div(r);
+      const char* p = src(t, h, a.rot_bytes + (r - h * (int)a.rest.d) * 16);
+      if (p != nullptr) x[0] = *reinterpret_cast<const uint4*>(p);
+    }, [&](int u, const uint4 (&x)[1]) {
+      const int t = (int)a.per_rest.div(u), r = u - t * (int)a.per_rest.d, h = (int)a.rest.div(r);
+      char* p = dst(t, h, a.rot_bytes + (r - h * (int)a.rest.d) * 16);
+      if (p != nullptr) *reinterpret_cast<uint4*>(p) = x[0];
+    });
   }
-  if (vd != nullptr) {
-    const int per = db / 16, n = G * per;
-    const int u1 = (int)((int64_t)n * (part + 1) / a.parts);
-#pragma unroll 4
-    for (int u = (int)((int64_t)n * part / a.parts) + lane; u < u1; u += 32) {
-      const int h = u / per, o = (u - h * per) * 16;
-      *reinterpret_cast<uint4*>(vd + h * a.pool.head_stride + o) = *reinterpret_cast<const uint4*>(vs + (int64_t)h * db + o);
-    }
-  }
+  each_item<2 * BATCH, 1>(nt * (int)a.per_v.d, [&](int u, uint4 (&x)[1]) {
+    const int t = (int)a.per_v.div(u), r = u - t * (int)a.per_v.d;
+    if (place[t] != -2) x[0] = *reinterpret_cast<const uint4*>(a.v + (t0 + t) * a.ldv + r * 16);
+  }, [&](int u, const uint4 (&x)[1]) {
+    const int t = (int)a.per_v.div(u), r = u - t * (int)a.per_v.d, h = r >> a.v_shift;
+    if (place[t] >= 0)
+      *reinterpret_cast<uint4*>(a.pool.v + place[t] + h * a.pool.head_stride + (r - (h << a.v_shift)) * 16) = x[0];
+  });
+}
+
+template <typename T>
+cudaError_t run_append(const AppendParams& a, dim3 grid, cudaStream_t st) {
+  return a.interleaved ? launch_pdl(paged_append_kernel<T, 1>, grid, dim3(kAppendThreads), 0, st, a)
+                       : launch_pdl(paged_append_kernel<T, 0>, grid, dim3(kAppendThreads), 0, st, a);
 }
 
 }  // namespace
@@ -175,14 +211,22 @@ cudaError_t launch_paged_append(const PagedAppendArgs& g, cudaStream_t st) {
   a.rot_bytes = g.rot_dim * es; a.interleaved = g.interleaved; a.pool = g.pool; a.status = g.status;
   for (int i = 0; i < g.rot_dim / 2; ++i)
     a.turns[i] = pow(g.rot_base, -2.0 * i / g.rot_dim) / (2.0 * M_PI);
-  // few tokens: several warps share one, until the GPU has 16 warps per SM or a warp has one chunk per lane left
+  const int heads = a.H + a.G, units = a.rot_bytes / 32, rest = (a.d_bytes - a.rot_bytes) / 16;
+  a.rot_units = FastDiv(units); a.per_rot = FastDiv(heads * units);
+  a.rest = FastDiv(rest); a.per_rest = FastDiv(heads * rest);
+  a.per_v = FastDiv(a.G * a.d_bytes / 16);
+  while ((16 << a.v_shift) < a.d_bytes) ++a.v_shift;
+  // many tokens: up to kMaxTok of them in a CTA, as long as there are eight CTAs per SM.  Few: a CTA each, and several
+  // CTAs share one until there are two per SM or 256 chunks for each.  (kMaxTok 1 / 4 / 8 / 16: 189 / 117 / 112 / 118 us on the
+  // prompts above.)
   const int64_t chunks = (int64_t)(a.H + 2 * a.G) * a.d_bytes / 16;
-  int64_t parts = (148 * 16 + g.n_tokens - 1) / g.n_tokens;
-  if (parts > (chunks + 31) / 32) parts = (chunks + 31) / 32;
-  a.parts = (int)(parts < 1 ? 1 : parts);
-  const int64_t blocks = ((int64_t)g.n_tokens * a.parts + 7) / 8;
-  return g.dtype == DT_F32 ? launch_pdl(paged_append_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, st, a)
-                           : launch_pdl(paged_append_kernel<bf16>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+  a.tok = g.n_tokens / (148 * 8);
+  a.tok = a.tok < 1 ? 1 : a.tok > kMaxTok ? kMaxTok : a.tok;
+  const int64_t groups = (g.n_tokens + a.tok - 1) / a.tok;
+  int64_t parts = (2 * 148 + groups - 1) / groups;
+  if (parts > (chunks + 255) / 256) parts = (chunks + 255) / 256;
+  const dim3 grid((unsigned)groups, (unsigned)(parts < 1 ? 1 : parts));
+  return g.dtype == DT_F32 ? run_append<float>(a, grid, st) : run_append<bf16>(a, grid, st);
 }
 
 int paged_pool_args(int es, int n_kv_heads, int d_kv, const void* k_pages, const void* v_pages, int n_pages, int page_size,
