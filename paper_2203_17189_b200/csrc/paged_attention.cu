@@ -42,6 +42,7 @@ struct AttnParams {
   float scale;
   int S, n_q, H, G, m;   // m = H / G query heads per kv head
   int tiles;             // tiles of query rows per kv head: ceil(n_q m / RT)
+  FastDiv by_m, by_tiles, by_items;      // divisions by m, by tiles, by the items of a sequence (G tiles)
   int cap;               // keys a page table row can name
   PagedPool pool;
   int runs;              // 1: pages hold whole runs of keys (KeyStream)
@@ -179,7 +180,7 @@ __device__ __forceinline__ int64_t key_offset(const AttnParams& a, const Place& 
     return -1;
   }
   return page * a.pool.page_stride + (j - pi * a.pool.page_size) * a.pool.slot_stride +
-         (p.k / a.tiles) * a.pool.head_stride;
+         a.by_tiles.div(p.k) * a.pool.head_stride;
 }
 
 // Shape of a warp's tiles: KT keys of DK columns of ES bytes, K then V, in a ring of STAGES.  4 KB of each where 32 lanes
@@ -273,10 +274,17 @@ template <typename L> struct KeyStream {
 // The query rows of an item and what is known of them
 struct Rows {
   int r0, n, g;      // first row of the tile, rows in it, kv head
-  __device__ __forceinline__ Rows(const AttnParams& a, const Place& p, int rt)
-      : r0((p.k % a.tiles) * rt), n(min(rt, a.n_q * a.m - (p.k % a.tiles) * rt)), g(p.k / a.tiles) {}
-  __device__ __forceinline__ int token(const AttnParams& a, const Place& p, int r) const { return p.s * a.n_q + (r0 + r) / a.m; }
-  __device__ __forceinline__ int head(const AttnParams& a, int r) const { return g * a.m + (r0 + r) % a.m; }
+  __device__ __forceinline__ Rows(const AttnParams& a, const Place& p, int rt) {
+    g = (int)a.by_tiles.div(p.k);
+    r0 = (p.k - g * a.tiles) * rt;
+    n = min(rt, a.n_q * a.m - r0);
+  }
+  // row of q and query head of row r of the tile
+  __device__ __forceinline__ void place(const AttnParams& a, const Place& p, int r, int& row, int& h) const {
+    const int t = (int)a.by_m.div(r0 + r);
+    row = p.s * a.n_q + t;
+    h = g * a.m + (r0 + r - t * a.m);
+  }
 };
 
 // Bookkeeping of a walk over a share: which piece an item's end leaves where
@@ -298,7 +306,7 @@ struct Pieces {
 // Where the rows of an item go
 __device__ __forceinline__ Place item_place(const AttnParams& a, int item) {
   Place p;
-  p.s = item / (a.G * a.tiles); p.k = item % (a.G * a.tiles); p.blk = p.nb = p.len = 0;
+  p.s = (int)a.by_items.div(item); p.k = item - p.s * (a.G * a.tiles); p.blk = p.nb = p.len = 0;
   return p;
 }
 template <typename T, int DK>
@@ -310,8 +318,8 @@ __device__ __forceinline__ void write_lse(const AttnParams& a, int row, int h, f
 }
 
 // End of a CTA: joins the pieces its warps left.  A chain of them that begins and ends here is an item's rows; one that
-// reaches beyond this CTA's first or last warp becomes the CTA's piece.  Chain w (-1: the one that comes in from the CTA
-// before) is taken by warp (w + 1) % 4.  Called by all threads.
+// reaches beyond this CTA's first or last warp becomes the CTA's piece.  The rows of all chains are dealt out to the warps.
+// Called by all threads.
 template <typename T, int DK, int RT>
 __device__ void finish_cta(const AttnParams& a, const int4& mine) {
   __shared__ int4 metas[kWarps];
@@ -321,9 +329,9 @@ __device__ void finish_cta(const AttnParams& a, const int4& mine) {
   constexpr int VC = DK / 32;
   const int64_t piece = (int64_t)a.rows * (DK + 2);
   const float* parts = a.warp_part + (int64_t)blockIdx.x * kWarps * 2 * piece;
-  if (tid == 0) a.meta[blockIdx.x] = make_int4(metas[0].x, 0, -1, 0);
-  __syncthreads();
-  for (int w = (tid >> 5) - 1; w < kWarps; w += kWarps) {
+  int4 meta = make_int4(metas[0].x, 0, -1, 0);
+  int turn = 0;      // rows seen so far: warp w takes those with turn % kWarps == w
+  for (int w = -1; w < kWarps; ++w) {
     // the chain that begins with warp w's slot 1, or (w = -1) with the first warp's slot 0
     const int item = w < 0 ? metas[0].x : metas[w].z;
     if (item < 0) continue;
@@ -332,18 +340,21 @@ __device__ void finish_cta(const AttnParams& a, const int4& mine) {
     while (goes_on && end + 1 < kWarps) goes_on = metas[++end].y != 0;
     const int n = end - w + (w < 0 ? 0 : 1);      // pieces: w < 0: slots 0 of warps 0 .. end; else slot 1 of w, slots 0 behind it
     const bool whole = w >= 0 && !goes_on;
-    if (lane == 0 && goes_on) (w < 0 ? a.meta[blockIdx.x].y : a.meta[blockIdx.x].z) = w < 0 ? 1 : item;
+    if (goes_on) { if (w < 0) meta.y = 1; else meta.z = item; }
     const Place p = item_place(a, item);
     const Rows rows(a, p, RT);
     const float* first = parts + (w < 0 ? 0 : 2 * w + 1) * piece;
     const int64_t second = w < 0 ? 2 * piece : piece;      // from the first piece to the one behind it; then 2 piece
 #pragma unroll 4
-    for (int r = 0; r < rows.n; ++r) {
-      float mx = -INFINITY, sum = 0.f, pm[kWarps], acc[VC];
+    for (int r = ((tid >> 5) - turn) & (kWarps - 1); r < rows.n; r += kWarps) {
+      float mx = -INFINITY, sum = 0.f, pm[kWarps], pl[kWarps], v[kWarps][VC], acc[VC];
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) {
         const float* q = first + (i == 0 ? 0 : second + (i - 1) * 2 * piece) + r * (DK + 2);
-        pm[i] = i < n ? q[DK] : -INFINITY;
+        pm[i] = -INFINITY; pl[i] = 0.f;
+        if (i < n) { pm[i] = q[DK]; pl[i] = q[DK + 1]; }
+#pragma unroll
+        for (int c = 0; c < VC; ++c) v[i][c] = i < n ? q[lane + 32 * c] : 0.f;
         mx = fmaxf(mx, pm[i]);
       }
       const float ref = mx == -INFINITY ? 0.f : mx;
@@ -351,16 +362,14 @@ __device__ void finish_cta(const AttnParams& a, const int4& mine) {
       for (int c = 0; c < VC; ++c) acc[c] = 0.f;
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) {
-        const float* q = first + (i == 0 ? 0 : second + (i - 1) * 2 * piece) + r * (DK + 2);
         const float e = ex2((pm[i] - ref) * kLog2e);
-        if (i < n) {
-          sum += e * q[DK + 1];
+        sum += e * pl[i];
 #pragma unroll
-          for (int c = 0; c < VC; ++c) acc[c] += e * q[lane + 32 * c];
-        }
+        for (int c = 0; c < VC; ++c) acc[c] += e * v[i][c];
       }
       if (whole) {
-        const int h = rows.head(a, r), row = rows.token(a, p, r);
+        int row, h;
+        rows.place(a, p, r, row, h);
 #pragma unroll
         for (int c = 0; c < VC; ++c) out_row<T, DK>(a, row, h)[lane + 32 * c] = from_f<T>(sum == 0.f ? 0.f : acc[c] / sum);
         if (lane == 0) write_lse(a, row, h, mx, sum);
@@ -371,7 +380,9 @@ __device__ void finish_cta(const AttnParams& a, const int4& mine) {
         if (lane == 0) { pt[DK] = mx; pt[DK + 1] = sum; }
       }
     }
+    turn += rows.n;
   }
+  if (tid == 0) a.meta[blockIdx.x] = meta;
 }
 
 __device__ __forceinline__ void report_length(const AttnParams& a, int row) {
@@ -407,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
 
   const int key_l = lane % L::KT, part_l = lane / L::KT;
   float m[RT], l[RT], o[RT][L::VC];
-  int len[RT];
+  int len[RT], head[RT], q_row[RT];
   bool fresh = true;
   int stage = 0;
   for (int64_t x = x0; x < x1; ++x) {
@@ -415,19 +426,32 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
     const int nr = rows.n;
     if (fresh) {
       fresh = false;
-      __syncwarp();
-      for (int idx = lane; idx < RT * DK; idx += 32) {
-        const int r = idx / DK;
-        qs[idx] = r < nr ? reinterpret_cast<const float*>(a.q + (int64_t)rows.token(a, cur, r) * a.ldq)[rows.head(a, r) * DK + idx % DK] : 0.f;
+      // lane r < nr looks its row up; the row's columns are then copied by all lanes
+      int row = 0, h = 0, row_keys = 0;
+      if (lane < nr) {
+        rows.place(a, cur, lane, row, h);
+        row_keys = row_len(a, row);
+        report_length(a, row);
       }
+      const int64_t at = (int64_t)row * a.ldq + (int64_t)h * DK * 4;
+      __syncwarp();
+      constexpr int PER = DK / 4;      // float4 of a row
+#pragma unroll
+      for (int i = 0; i < (RT * PER + 31) / 32; ++i) {
+        const int idx = i * 32 + lane, r = idx / PER;
+        const int64_t o = __shfl_sync(0xffffffffu, at, r & 31);
+        if (r < nr) reinterpret_cast<float4*>(qs)[idx] = *reinterpret_cast<const float4*>(a.q + o + (idx % PER) * 16);
+      }
+      __syncwarp();
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         m[r] = -INFINITY; l[r] = 0.f;
-        len[r] = r < nr ? row_len(a, rows.token(a, cur, r)) : 0;
+        len[r] = __shfl_sync(0xffffffffu, row_keys, r);
+        head[r] = __shfl_sync(0xffffffffu, h, r);
+        q_row[r] = __shfl_sync(0xffffffffu, row, r);
 #pragma unroll
         for (int c = 0; c < L::VC; ++c) o[r][c] = 0.f;
       }
-      if (lane < nr) report_length(a, rows.token(a, cur, lane));
     }
     cp_async_wait<L::STAGES - 2>();
     __syncwarp();
@@ -460,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
           for (int of = L::KT; of < 32; of <<= 1) sc[r] += __shfl_xor_sync(0xffffffffu, sc[r], of);
           const bool seen = ((ok >> key_l) & 1) && j < len[r];
           float s = sc[r] * a.scale;
-          if (a.bias != nullptr && seen) s += a.bias[(int64_t)rows.head(a, r) * a.n_bias + max(a.n_bias - len[r] + j, 0)];
+          if (a.bias != nullptr && seen) s += a.bias[(int64_t)head[r] * a.n_bias + max(a.n_bias - len[r] + j, 0)];
           s = seen ? s : -INFINITY;
           float mx = s;
 #pragma unroll
@@ -505,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
 #pragma unroll
           for (int of = 16; of > 0; of >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
           const bool whole = pieces.whole(item_ends);
-          const int h = rows.head(a, r), row = rows.token(a, cur, r);
+          const int h = head[r], row = q_row[r];
           float* at = whole ? out_row<float, DK>(a, row, h) : part + (pieces.slot() * a.rows + r) * (DK + 2);
 #pragma unroll
           for (int c = 0; c < L::VC; ++c) at[lane * L::VC + c] = !whole ? o[r][c] : (lt == 0.f ? 0.f : o[r][c] / lt);
@@ -624,8 +648,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_mma_kernel(const __gri
         m[hf] = -INFINITY; l[hf] = 0.f; len[hf] = 0; far[hf] = 0.f; bias[hf] = nullptr;
         const uint32_t* src = nullptr;
         if (valid) {
-          const int row = rows.token(a, cur, r), h = rows.head(a, r);
+          int row, h;
+          rows.place(a, cur, r, row, h);
           len[hf] = row_len(a, row);
+          if (quad == 0) report_length(a, row);
           min_len = min(min_len, len[hf]); max_len = max(max_len, len[hf]);
           src = reinterpret_cast<const uint32_t*>(a.q + (int64_t)row * a.ldq + h * (DK * 2)) + quad;
           if (a.bias != nullptr) { bias[hf] = a.bias + (int64_t)h * a.n_bias; far[hf] = bias[hf][0]; }
@@ -645,7 +671,6 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_mma_kernel(const __gri
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < CN; ++i) o[t][i] = 0.f;
-      if (lane < rows.n) report_length(a, rows.token(a, cur, lane));
     }
     cp_async_wait<L::STAGES - 2>();
     __syncwarp();
@@ -795,7 +820,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_mma_kernel(const __gri
         const int r = lane / 4 + 8 * hf;
         if (r < rows.n) {
           if (whole) {
-            const int h = rows.head(a, r), row = rows.token(a, cur, r);
+            int row, h;
+            rows.place(a, cur, r, row, h);
             bf16* at = out_row<bf16, DK>(a, row, h) + quad * 2;
             const float inv = lt == 0.f ? 0.f : 1.f / lt;
 #pragma unroll
@@ -845,38 +871,48 @@ __global__ void __launch_bounds__(128) paged_attn_join_kernel(const __grid_const
   auto piece = [&](int i) {
     return a.part + (((int64_t)(c0 + i) * 2 + (i == 0 ? 1 : 0)) * a.rows + r) * (DK + 2);
   };
-  // four warps take every fourth piece; a lane holds DK / 32 columns
-  constexpr int VC = DK / 32;
-  __shared__ float red[4][DK + 2];
-  float mx = -INFINITY, sum = 0.f, acc[VC];
-#pragma unroll
-  for (int c = 0; c < VC; ++c) acc[c] = 0.f;
-  for (int i = w; i < n; i += 4) {
-    const float* pt = piece(i);
-    const float pm = pt[DK], ps = pt[DK + 1];
-    const float nm = fmaxf(mx, pm), ref = nm == -INFINITY ? 0.f : nm;
-    const float f0 = ex2((mx - ref) * kLog2e), f1 = ex2((pm - ref) * kLog2e);
-    sum = sum * f0 + ps * f1;
-#pragma unroll
-    for (int c = 0; c < VC; ++c) acc[c] = acc[c] * f0 + pt[lane * VC + c] * f1;
-    mx = nm;
+  // the weights of all pieces first, then their columns: every load of a pass is independent of the others
+  __shared__ float weight[kMaxCtas], top[4], sums[4];
+  float mx = -INFINITY;
+  for (int i = tid; i < n; i += 128) {
+    weight[i] = piece(i)[DK];
+    mx = fmaxf(mx, weight[i]);
   }
 #pragma unroll
-  for (int c = 0; c < VC; ++c) red[w][lane * VC + c] = acc[c];
-  if (lane == 0) { red[w][DK] = mx; red[w][DK + 1] = sum; }
+  for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  if (lane == 0) top[w] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  float sum = 0.f;
+  for (int i = tid; i < n; i += 128) {
+    weight[i] = ex2((weight[i] - ref) * kLog2e);
+    sum += weight[i] * piece(i)[DK + 1];
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) sums[w] = sum;
+  __syncthreads();
+  sum = sums[0] + sums[1] + sums[2] + sums[3];
+  // four warps take every fourth piece; a lane holds DK / 32 columns
+  constexpr int VC = DK / 32;
+  __shared__ float red[4][DK];
+  float acc[VC];
+#pragma unroll
+  for (int c = 0; c < VC; ++c) acc[c] = 0.f;
+#pragma unroll 8
+  for (int i = w; i < n; i += 4) {
+    const float* pt = piece(i);
+#pragma unroll
+    for (int c = 0; c < VC; ++c) acc[c] += weight[i] * pt[lane + 32 * c];
+  }
+#pragma unroll
+  for (int c = 0; c < VC; ++c) red[w][lane + 32 * c] = acc[c];
   __syncthreads();
   if (tid < DK) {
-    mx = fmaxf(fmaxf(red[0][DK], red[1][DK]), fmaxf(red[2][DK], red[3][DK]));
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    float v = 0.f;
-    sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float e = ex2((red[i][DK] - ref) * kLog2e);
-      v += e * red[i][tid];
-      sum += e * red[i][DK + 1];
-    }
-    const int h = rows.head(a, r), row = rows.token(a, p, r);
+    const float v = red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid];
+    int row, h;
+    rows.place(a, p, r, row, h);
     out_row<T, DK>(a, row, h)[tid] = from_f<T>(sum == 0.f ? 0.f : v / sum);
     if (tid == 0) write_lse(a, row, h, mx, sum);
   }
@@ -915,6 +951,7 @@ cudaError_t run_attention(AttnParams& a, Kernel kernel, int smem, cudaStream_t s
   if (e != cudaSuccess) return e;
   a.tiles = (a.n_q * a.m + RT - 1) / RT;
   a.rows = a.n_q * a.m < RT ? a.n_q * a.m : RT;
+  a.by_m = FastDiv(a.m); a.by_tiles = FastDiv(a.tiles); a.by_items = FastDiv(a.G * a.tiles);
   e = launch_pdl(kernel, dim3(ctas), dim3(kThreads), (size_t)smem, st, a);
   if (e != cudaSuccess) return e;
   return launch_pdl(paged_attn_join_kernel<T, DK, RT>, dim3(ctas - 1, a.rows), dim3(128), 0, st, a, ctas);
