@@ -27,8 +27,9 @@
 namespace {
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kMaxCtas = 296;      // 148 SMs, two CTAs each (the rings take 96 KB)
-constexpr int kMaxWorkers = kMaxCtas * kWarps;
+// CTAs of a grid at most: 148 SMs, two CTAs each (their rings take 96 KB), four with the smaller rings of narrow heads
+constexpr int max_ctas(int d_kv) { return 148 * (d_kv <= 32 ? 4 : 2); }
+constexpr int kMaxCtas = max_ctas(32);
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttnParams {
@@ -461,9 +462,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
     if (ok != 0) {
       const unsigned char* kt = keys.ring + stage * 2 * L::BYTES;
       const unsigned char* vt = kt + L::BYTES;
-      float sc[RT];
+      float sc[RT], add[RT];
 #pragma unroll
-      for (int r = 0; r < RT; ++r) sc[r] = 0.f;
+      for (int r = 0; r < RT; ++r) {
+        sc[r] = add[r] = 0.f;
+        if (a.bias != nullptr && j < len[r]) add[r] = a.bias[(int64_t)head[r] * a.n_bias + max(a.n_bias - len[r] + j, 0)];
+      }
 #pragma unroll
       for (int c = 0; c < L::CL; ++c) {
         const int ch = part_l * L::CL + c;
@@ -483,9 +487,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
 #pragma unroll
           for (int of = L::KT; of < 32; of <<= 1) sc[r] += __shfl_xor_sync(0xffffffffu, sc[r], of);
           const bool seen = ((ok >> key_l) & 1) && j < len[r];
-          float s = sc[r] * a.scale;
-          if (a.bias != nullptr && seen) s += a.bias[(int64_t)head[r] * a.n_bias + max(a.n_bias - len[r] + j, 0)];
-          s = seen ? s : -INFINITY;
+          const float s = seen ? fmaf(sc[r], a.scale, add[r]) : -INFINITY;
           float mx = s;
 #pragma unroll
           for (int of = 16; of > 0; of >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, of));
@@ -612,7 +614,7 @@ __device__ __noinline__ void values_by_key(const unsigned char* vt, const float*
 }
 
 template <int DK, int RT>
-__global__ void __launch_bounds__(kThreads, 2) paged_attn_mma_kernel(const __grid_constant__ AttnParams a) {
+__global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_kernel(const __grid_constant__ AttnParams a) {
   pdl_sync();
   using L = Mma<DK, RT>;
   constexpr bool H16 = RT == 16;
@@ -935,7 +937,7 @@ cudaError_t grid_of(Kernel kernel, int smem, int* ctas) {
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, smem);
     if (e != cudaSuccess) return e;
-    n = sms * per_sm < kMaxCtas ? sms * per_sm : kMaxCtas;
+    n = sms * per_sm < max_ctas(DK) ? sms * per_sm : max_ctas(DK);
     if (n < 2) n = 2;
     known[dev].store(n, std::memory_order_release);
   }
@@ -972,7 +974,8 @@ template <int DK> cudaError_t run_bf16(AttnParams& a, cudaStream_t st) {
 int64_t paged_attention_workspace(int n_rows, int n_q, int H, int Hkv, int d_kv) {
   (void)n_rows;
   const int64_t all = (int64_t)n_q * (H / Hkv), rows = all < 16 ? all : 16;
-  return kMaxCtas * (int64_t)sizeof(int4) + (kMaxCtas + kMaxWorkers) * 2 * rows * (d_kv + 2) * 4;
+  const int64_t ctas = max_ctas(d_kv);
+  return ctas * (int64_t)sizeof(int4) + ctas * (1 + kWarps) * 2 * rows * (d_kv + 2) * 4;
 }
 
 cudaError_t launch_paged_attention(const PagedAttnArgs& g, cudaStream_t st) {
@@ -987,8 +990,8 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& g, cudaStream_t st) {
   a.pool = g.pool; a.status = g.status;
   a.meta = (int4*)g.workspace;
   const int rows = a.n_q * a.m < 16 ? a.n_q * a.m : 16;
-  a.part = (float*)((char*)g.workspace + kMaxCtas * sizeof(int4));
-  a.warp_part = a.part + (int64_t)kMaxCtas * 2 * rows * (g.d_kv + 2);
+  a.part = (float*)((char*)g.workspace + max_ctas(g.d_kv) * sizeof(int4));
+  a.warp_part = a.part + (int64_t)max_ctas(g.d_kv) * 2 * rows * (g.d_kv + 2);
   if (g.dtype == DT_F32) return g.d_kv == 32 ? run_f32<32>(a, st) : g.d_kv == 64 ? run_f32<64>(a, st) : run_f32<128>(a, st);
   return g.d_kv == 32 ? run_bf16<32>(a, st) : g.d_kv == 64 ? run_bf16<64>(a, st) : run_bf16<128>(a, st);
 }
