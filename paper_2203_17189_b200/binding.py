@@ -380,86 +380,41 @@ def t5_selftest_bounded_wait(status, limit_cycles):
     _check(lib().t5_selftest_bounded_wait(_ptr(status), int(limit_cycles), _stream()))
 
 
-# ---- serving.  A call here takes some microseconds on the GPU, so the host side is kept to about as many: pointers and
-# sizes go to ctypes as plain ints, and what a wrong tensor would turn into an access out of range (type, shape, place) is
-# tested in one expression per call; only when that fails is the culprit looked for.
+# ---- serving.  A call takes some microseconds on the GPU, so its host side is native too (csrc/py_serving.cpp): tensors
+# are checked and marshalled there; here are the names, the defaults and the errors.
 
-_CODES = {torch.float32: 0, torch.bfloat16: 1}
-_I32, _F32 = torch.int32, torch.float32
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_serving = None
 
 
-def _refuse(device, checks):
-    """Raises for the first tensor that is not (name, tensor, dtype, shape) with a contiguous last dimension on the
-    current device."""
-    for name, t, dtype, shape in checks:
-        if t is None:
-            raise T5Error(-8, f"{name} is missing")
-        if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.get_device() != device or (
-                t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1):
-            raise T5Error(-8, f"{name}: want a {dtype} tensor {tuple(shape)} on the current device {device} with a contiguous "
-                              f"last dimension, got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
-    raise T5Error(-8, "tensors: heads must be adjacent columns, both pools alike in their strides, vectors contiguous, all "
-                      "on the current CUDA device")
+def _native():
+    global _serving
+    if _serving is None:
+        L = lib()
+        try:
+            from . import _serving as module
+        except ImportError as e:
+            raise RuntimeError("the serving calls' Python module is missing: run `python -m paper_2203_17189_b200.build` "
+                               "(or __graft_entry__.build()) first") from e
+        module.bind(*(C.cast(f, C.c_void_p).value for f in (L.t5_paged_kv_append, L.t5_paged_attention, L.t5_verify_draft)))
+        _serving = module
+    return _serving
 
 
-def _row_stride(t, shape, d):
-    """Row stride of [rows, heads, d] with adjacent heads, or -1; rows may be slices of wider ones."""
-    st = t.stride()
-    if st[2] != 1 or (st[1] != d and shape[1] > 1):
-        return -1
-    return st[0] if shape[0] > 1 else shape[1] * d
-
-
-def _pool_strides(k_pages, v_pages, shape):
-    """Strides of both pools (a dimension of one entry has none), or None if they differ."""
-    sk, sv = k_pages.stride(), v_pages.stride()
-    if sk == sv and sk[3] == 1 and 1 not in shape:
-        return sk[0], sk[1], sk[2]
-    n, ps, g, d = shape
-    if sk[3] != 1 or sv[3] != 1 or any(sk[i] != sv[i] and shape[i] > 1 for i in range(3)):
-        return None
-    return tuple(sk[i] if shape[i] > 1 else ps * g * d for i in range(3))
+def _raise(r):
+    if isinstance(r, str):
+        raise T5Error(-8, r)
+    _check(r)
 
 
 def t5_paged_kv_append(k, v, k_pages, v_pages, page_table, seq_of_token, positions, q=None, q_out=None, rot_dim=0,
                        rot_base=10000.0, rot_interleaved=False):
     """k, v [tokens, kv_heads, d_kv] (and q [tokens, heads, d_kv] into q_out) enter the pools [n_pages, page_size,
-    kv_heads, d_kv]; see the header."""
-    dt, dev = k.dtype, k.get_device()
-    if k.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2 or dt not in _CODES or (q is None) != (q_out is None):
-        raise T5Error(-8, "want float32 or bfloat16 k [tokens, kv_heads, d_kv], pools [n_pages, page_size, kv_heads, d_kv], a "
-                          "2-D page table, and q with q_out")
-    shape, ps, table = k.shape, k_pages.shape, page_table.shape
-    n, g, d = shape
-    ldk, ldv, st = _row_stride(k, shape, d), _row_stride(v, shape, d) if v.shape == shape else -1, page_table.stride()
-    pool = _pool_strides(k_pages, v_pages, ps) if v_pages.shape == ps else None
-    h = ldq = ldqo = qp = qop = 0
-    fine = True
-    if q is not None:
-        qs = q.shape
-        fine = len(qs) == 3 and qs[0] == n and qs[2] == d and q_out.shape == qs and q.dtype is dt and q_out.dtype is dt and \
-            q.get_device() == dev and q_out.get_device() == dev
-        if fine:
-            h, ldq, ldqo, qp, qop = qs[1], _row_stride(q, qs, d), _row_stride(q_out, qs, d), q.data_ptr(), q_out.data_ptr()
-    if not (fine and ldk >= 0 and ldv >= 0 and ldq >= 0 and ldqo >= 0 and pool and ps[2] == g and ps[3] == d and v.dtype is dt
-            and k_pages.dtype is dt and v_pages.dtype is dt and page_table.dtype is _I32 and seq_of_token.dtype is _I32
-            and positions.dtype is _I32 and seq_of_token.numel() == n and positions.numel() == n and st[1] == 1
-            and seq_of_token.is_contiguous() and positions.is_contiguous()
-            and dev == v.get_device() == k_pages.get_device() == v_pages.get_device() == page_table.get_device()
-            == seq_of_token.get_device() == positions.get_device() == torch.cuda.current_device()):
-        heads = None if q is None else (n, q.shape[1], d)
-        _refuse(torch.cuda.current_device(), [
-            ("k", k, dt, shape), ("v", v, dt, shape), ("k_pages", k_pages, dt, (ps[0], ps[1], g, d)),
-            ("v_pages", v_pages, dt, ps), ("page_table", page_table, _I32, table), ("seq_of_token", seq_of_token, _I32, (n,)),
-            ("positions", positions, _I32, (n,))] + ([] if q is None else [("q", q, dt, heads), ("q_out", q_out, dt, heads)]))
-    rc = lib().t5_paged_kv_append(_CODES[dt], n, h, g, d, qp, ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, qop, ldqo,
-                                  seq_of_token.data_ptr(), positions.data_ptr(), rot_dim, rot_base, int(rot_interleaved),
-                                  k_pages.data_ptr(), v_pages.data_ptr(), ps[0], ps[1], *pool, page_table.data_ptr(), table[0],
-                                  table[1], st[0] if table[0] > 1 else table[1], _raw_stream(dev))
-    if rc:
-        _check(rc)
+    kv_heads, d_kv] (any strides, the same for both); page_table [sequences, pages], seq_of_token / positions [tokens]
+    int32; see the header."""
+    r = (_serving or _native()).paged_kv_append(k, v, k_pages, v_pages, page_table, seq_of_token, positions, q, q_out, rot_dim,
+                                                rot_base, rot_interleaved)
+    if r is not None:
+        _raise(r)
 
 
 def t5_paged_attention_workspace_bytes(n_rows, n_q, n_heads, n_kv_heads, d_kv):
@@ -469,79 +424,16 @@ def t5_paged_attention_workspace_bytes(n_rows, n_q, n_heads, n_kv_heads, d_kv):
 
 
 def t5_paged_attention(q, k_pages, v_pages, page_table, lens, out, workspace, scale=1.0, n_q=1, bias=None, lse=None):
-    """q, out [rows, heads, d_kv]; lens [rows]; n_q rows per row of the page table; bias [heads, n_bias] float32, the
+    """q, out [rows, heads, d_kv]; lens [rows] int32; n_q rows per row of the page table; bias [heads, n_bias] float32, the
     near end last; lse [rows, heads] float32; see the header."""
-    dt, dev = q.dtype, q.get_device()
-    if q.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2 or dt not in _CODES or (bias is not None and bias.dim() != 2):
-        raise T5Error(-8, "want float32 or bfloat16 q [rows, heads, d_kv], pools [n_pages, page_size, kv_heads, d_kv], a 2-D "
-                          "page table, a 2-D bias")
-    shape, ps, table = q.shape, k_pages.shape, page_table.shape
-    r, h, d = shape
-    g = ps[2]
-    ldq, ldo, st = _row_stride(q, shape, d), _row_stride(out, shape, d) if out.shape == shape else -1, page_table.stride()
-    pool = _pool_strides(k_pages, v_pages, ps) if v_pages.shape == ps else None
-    n_bias = bp = lp = 0
-    fine = True
-    if bias is not None:
-        n_bias, bp = bias.shape[1], bias.data_ptr()
-        fine = bias.shape[0] == h and bias.dtype is _F32 and bias.is_contiguous() and bias.get_device() == dev
-    if lse is not None:
-        lp = lse.data_ptr()
-        fine = fine and lse.shape == shape[:2] and lse.dtype is _F32 and lse.is_contiguous() and lse.get_device() == dev
-    if not (fine and ldq >= 0 and ldo >= 0 and pool and ps[3] == d and table[0] * n_q == r and st[1] == 1 and out.dtype is dt
-            and k_pages.dtype is dt and v_pages.dtype is dt and page_table.dtype is _I32 and lens.dtype is _I32
-            and lens.numel() == r and lens.is_contiguous() and workspace.is_contiguous()
-            and dev == out.get_device() == k_pages.get_device() == v_pages.get_device() == page_table.get_device()
-            == lens.get_device() == workspace.get_device() == torch.cuda.current_device()):
-        _refuse(torch.cuda.current_device(), [
-            ("q", q, dt, shape), ("out", out, dt, shape), ("k_pages", k_pages, dt, (ps[0], ps[1], g, d)),
-            ("v_pages", v_pages, dt, ps), ("page_table (n_q rows of q per row)", page_table, _I32, (r // max(n_q, 1), table[1])),
-            ("lens", lens, _I32, (r,)), ("workspace", workspace, workspace.dtype, workspace.shape)]
-            + ([] if bias is None else [("bias", bias, _F32, (h, n_bias))]) + ([] if lse is None else [("lse", lse, _F32, (r, h))]))
-    rc = lib().t5_paged_attention(_CODES[dt], r, n_q, h, g, d, scale, q.data_ptr(), ldq, k_pages.data_ptr(),
-                                  v_pages.data_ptr(), ps[0], ps[1], *pool, page_table.data_ptr(), table[1],
-                                  st[0] if table[0] > 1 else table[1], lens.data_ptr(), bp, n_bias, out.data_ptr(), ldo, lp,
-                                  workspace.data_ptr(), workspace.nbytes, _raw_stream(dev))
-    if rc:
-        _check(rc)
+    r = (_serving or _native()).paged_attention(q, k_pages, v_pages, page_table, lens, out, workspace, scale, n_q, bias, lse)
+    if r is not None:
+        _raise(r)
 
 
 def t5_verify_draft(target, draft, draft_tokens, n_draft, u_accept, u_sample, out_tokens, n_accepted):
     """target [seqs, drafts + 1, vocab], draft [seqs, drafts, vocab] or None, draft_tokens / u_accept [seqs, drafts],
     n_draft [seqs] or None, u_sample [seqs] -> out_tokens [seqs, drafts + 1], n_accepted [seqs]; see the header."""
-    dt, dev = target.dtype, target.get_device()
-    if target.dim() != 3 or target.shape[1] < 1 or dt not in _CODES:
-        raise T5Error(-8, "target: want float32 or bfloat16 [seqs, drafts + 1, vocab]")
-    s, k1, v = target.shape
-    k = k1 - 1
-    tt, tx, tu, to = target.stride(), draft_tokens.stride(), u_accept.stride(), out_tokens.stride()
-    np_ = dp = ds = 0
-    dr = v
-    fine = True
-    if n_draft is not None:
-        np_ = n_draft.data_ptr()
-        fine = n_draft.dtype is _I32 and n_draft.numel() == s and n_draft.is_contiguous() and n_draft.get_device() == dev
-    if draft is not None and k > 0:
-        td, dp = draft.stride(), draft.data_ptr()
-        fine = fine and draft.dtype is dt and draft.shape == (s, k, v) and (td[2] == 1 or v == 1) and draft.get_device() == dev
-        if fine:
-            ds, dr = td[0] if s > 1 else 0, td[1] if k > 1 else v
-    if not (fine and (tt[2] == 1 or v == 1) and draft_tokens.shape == (s, k) and u_accept.shape == (s, k)
-            and out_tokens.shape == (s, k1) and (k <= 1 or (tx[1] == 1 and tu[1] == 1)) and (k == 0 or to[1] == 1)
-            and draft_tokens.dtype is _I32 and u_accept.dtype is _F32 and u_sample.dtype is _F32 and out_tokens.dtype is _I32
-            and n_accepted.dtype is _I32 and u_sample.numel() == s and n_accepted.numel() == s and u_sample.is_contiguous()
-            and n_accepted.is_contiguous()
-            and dev == draft_tokens.get_device() == u_accept.get_device() == u_sample.get_device() == out_tokens.get_device()
-            == n_accepted.get_device() == torch.cuda.current_device()):
-        _refuse(torch.cuda.current_device(), [
-            ("target", target, dt, (s, k1, v)), ("draft_tokens", draft_tokens, _I32, (s, k)), ("u_accept", u_accept, _F32, (s, k)),
-            ("u_sample", u_sample, _F32, (s,)), ("out_tokens", out_tokens, _I32, (s, k1)), ("n_accepted", n_accepted, _I32, (s,))]
-            + ([] if draft is None else [("draft", draft, dt, (s, k, v))])
-            + ([] if n_draft is None else [("n_draft", n_draft, _I32, (s,))]))
-    one = s <= 1
-    rc = lib().t5_verify_draft(_CODES[dt], s, k, v, target.data_ptr(), 0 if one else tt[0], tt[1] if k else v, dp, ds, dr,
-                               draft_tokens.data_ptr(), k if one else tx[0], np_, u_accept.data_ptr(), k if one else tu[0],
-                               u_sample.data_ptr(), out_tokens.data_ptr(), k1 if one else to[0], n_accepted.data_ptr(),
-                               _raw_stream(dev))
-    if rc:
-        _check(rc)
+    r = (_serving or _native()).verify_draft(target, draft, draft_tokens, n_draft, u_accept, u_sample, out_tokens, n_accepted)
+    if r is not None:
+        _raise(r)

@@ -11,6 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libt5b200.so")
+PY_LIB = os.path.join(HERE, "_serving.so")      # Python side of the serving calls (csrc/py_serving.cpp)
 SOURCES = ["t5_model.cu", "elementwise.cu", "gemm_simt.cu", "gemm_tcgen05.cu", "attention_simt.cu", "attention_tc.cu",
            "relbias.cu", "noalloc.cu", "selftest.cu", "paged_append.cu", "paged_attention.cu", "verify_draft.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
@@ -31,6 +32,17 @@ def _stale(target, deps):
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _python_module_command():
+    import sysconfig
+
+    from torch.utils.cpp_extension import include_paths, library_paths
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           os.path.join(CSRC, "py_serving.cpp"), "-o", PY_LIB, "-I" + sysconfig.get_paths()["include"],
+           "-I" + os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")]
+    cmd += ["-isystem" + p for p in include_paths()]
+    return cmd + ["-L" + p for p in library_paths()] + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+
+
 def build(force=False, verbose=False):
     os.makedirs(OBJ, exist_ok=True)
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
@@ -45,6 +57,10 @@ def build(force=False, verbose=False):
         if force or _stale(o, [s] + headers):
             jobs.append([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", s, "-o", o])
 
+    py_deps = [os.path.join(CSRC, "py_serving.cpp"), headers[-1]]
+    if force or _stale(PY_LIB, py_deps):
+        jobs.append(_python_module_command())
+
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         return cmd, r
@@ -53,8 +69,8 @@ def build(force=False, verbose=False):
             if verbose or r.returncode != 0:
                 sys.stderr.write(r.stdout + r.stderr)
             if r.returncode != 0:
-                raise RuntimeError("nvcc failed: " + " ".join(cmd))
-    if jobs or not os.path.exists(LIB):
+                raise RuntimeError("compiler failed: " + " ".join(cmd))
+    if any(c[0] == nvcc for c in jobs) or not os.path.exists(LIB):
         cmd = [nvcc, "-shared", "-o", LIB] + objs + ["-gencode", "arch=compute_100a,code=sm_100a",
                                                       "-cudart", "static"]
         r = subprocess.run(cmd, capture_output=True, text=True)
