@@ -20,9 +20,12 @@
 #include "../../include/t5_b200.h"
 #include "paged.cuh"
 
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include <atomic>
+
+namespace cg = cooperative_groups;
 
 namespace {
 
@@ -43,13 +46,14 @@ struct AttnParams {
   float scale;
   int S, n_q, H, G, m;   // m = H / G query heads per kv head
   int tiles;             // tiles of query rows per kv head: ceil(n_q m / RT)
-  FastDiv by_m, by_tiles, by_items;      // divisions by m, by tiles, by the items of a sequence (G tiles)
+  FastDiv by_m, by_tiles, by_items, by_workers;      // divisions by m, tiles, the items of a sequence (G tiles), the warps
   int cap;               // keys a page table row can name
   PagedPool pool;
   int runs;              // 1: pages hold whole runs of keys (KeyStream)
   float* warp_part;      // [workers][2][rows][d + 2]: output, maximum, sum of the pieces a warp leaves
   float* part;           // [ctas][2][rows][d + 2]: the same of a CTA
   int4* meta;            // [ctas]: which pieces those are, see below
+  int cluster;           // CTAs per item when every item has a cluster of its own
   int rows;              // query rows of a slot: min(RT, n_q m)
   int* status;
 };
@@ -103,6 +107,9 @@ __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1
     const int n = blocks_of(seq_len(a, s), bk);
     if (s == tid) first = n;
     mine += n;
+    if (blockIdx.x == 0)
+      for (int i = 0; i < a.n_q; ++i)
+        if (a.lens[s * a.n_q + i] > a.cap) paged_report(a.status, PAGED_BAD_LENGTH);
   }
   const int64_t ws = warp_sum64(mine);
   if (lane == 0) sums[w] = ws;
@@ -112,14 +119,20 @@ __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1
   for (int i = 0; i < kWarps; ++i) total += sums[i];
   const int64_t items = (int64_t)a.G * a.tiles, n_w = (int64_t)gridDim.x * kWarps;
   total *= items;
+  // share c: [c q + min(c, r), ...) with total = q n_w + r, so fewer tiles than warps leave the last warps without work.
+  // Lane i looks at the CTA's i-th share; a division of 64 bits takes as long as a memory access and is left to huge totals.
+  const bool small = total < (1ll << 31);
+  const int64_t q = small ? (int64_t)a.by_workers.div((uint32_t)total) : total / n_w, rest = total - q * n_w;
+  const int64_t c = (int64_t)blockIdx.x * kWarps + min(lane, kWarps);
+  const int64_t begin = c * q + min(c, rest);
+  const int64_t mine_at = small ? (int64_t)a.by_items.div((uint32_t)begin) : begin / items;
+  x0 = __shfl_sync(0xffffffffu, begin, w);
+  x1 = __shfl_sync(0xffffffffu, begin, w + 1);
   int64_t at[kWarps];      // where the warps' shares begin, in tiles of one item per sequence (-1: no share)
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) {
-    const int64_t c = (int64_t)blockIdx.x * kWarps + i;
-    // fewer tiles than warps: the warps without work lie behind all others
-    const int64_t b0 = total >= n_w ? total * c / n_w : min(c, total), b1 = total >= n_w ? total * (c + 1) / n_w : min(c + 1, total);
-    at[i] = b0 < b1 ? b0 / items : -1;
-    if (i == w) { x0 = b0; x1 = b1; }
+    const int64_t v = __shfl_sync(0xffffffffu, mine_at, i);
+    at[i] = __shfl_sync(0xffffffffu, begin, i) < __shfl_sync(0xffffffffu, begin, i + 1) ? v : -1;
   }
   // the sequence whose tiles hold x0: prefix(s) <= x0 / items < prefix(s + 1)
   int64_t base = 0;
@@ -152,7 +165,7 @@ __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1
   p.len = seq_len(a, p.s);
   p.nb = blocks_of(p.len, bk);
   const int64_t in = x0 - found_prefix[w] * items;
-  p.k = (int)(in / p.nb);
+  p.k = small ? (int)((uint32_t)in / (uint32_t)p.nb) : (int)(in / p.nb);
   p.blk = (int)(in - (int64_t)p.k * p.nb);
 }
 
@@ -386,8 +399,51 @@ __device__ void finish_cta(const AttnParams& a, const int4& mine) {
   if (tid == 0) a.meta[blockIdx.x] = meta;
 }
 
-__device__ __forceinline__ void report_length(const AttnParams& a, int row) {
-  if (a.lens[row] > a.cap) paged_report(a.status, PAGED_BAD_LENGTH);
+// Short caches and few items: a cluster of a.cluster CTAs per item instead of shares of the line.  Its warps take equal
+// runs of the item's tiles and join through distributed shared memory, which spares the second kernel and the search.
+__device__ __forceinline__ void cluster_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1, Place& p) {
+  const int item = blockIdx.x / a.cluster, n = a.cluster * kWarps;
+  const int w = (blockIdx.x - item * a.cluster) * kWarps + (threadIdx.x >> 5);
+  p = item_place(a, item);
+  p.len = seq_len(a, p.s);
+  p.nb = blocks_of(p.len, bk);
+  x0 = p.nb * w / n;
+  x1 = p.nb * (w + 1) / n;
+  p.blk = (int)x0;
+  if (blockIdx.x == item * a.cluster && p.k == 0 && threadIdx.x < a.n_q && a.lens[p.s * a.n_q + threadIdx.x] > a.cap)
+    paged_report(a.status, PAGED_BAD_LENGTH);
+}
+// Joins the warps of a cluster: warp w of each CTA has left its rows ([row][DK + 2]: output, maximum, sum) at smem + w *
+// stride.  A warp of the cluster takes 32 columns of a row; lane i looks at piece i's maximum and sum.
+template <typename T, int DK, int RT>
+__device__ void finish_cluster(const AttnParams& a, const Place& p, unsigned char* smem, int stride) {
+  cg::cluster_group cluster = cg::this_cluster();
+  cluster.sync();
+  const Rows rows(a, p, RT);
+  const int lane = threadIdx.x & 31, n = a.cluster * kWarps;      // at most 32 pieces
+  const int rank = (int)cluster.block_rank();
+  for (int unit = rank * kWarps + (threadIdx.x >> 5); unit < rows.n * (DK / 32); unit += n) {
+    const int r = unit / (DK / 32), c = unit % (DK / 32) * 32 + lane;
+    auto piece = [&](int i) {
+      return reinterpret_cast<const float*>(cluster.map_shared_rank(smem + (i % kWarps) * stride, i / kWarps)) + r * (DK + 2);
+    };
+    float m = -INFINITY, l = 0.f;
+    if (lane < n) { m = piece(lane)[DK]; l = piece(lane)[DK + 1]; }
+    float mx = m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float e = ex2((m - (mx == -INFINITY ? 0.f : mx)) * kLog2e);
+    float sum = e * l, acc = 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) acc += __shfl_sync(0xffffffffu, e, i) * piece(i)[c];
+    int row, h;
+    rows.place(a, p, r, row, h);
+    out_row<T, DK>(a, row, h)[c] = from_f<T>(sum == 0.f ? 0.f : acc / sum);
+    if (c == 0) write_lse(a, row, h, mx, sum);
+  }
+  cluster.sync();      // nobody leaves while its shared memory is read
 }
 
 // ------------------------------------------------------------------ float32: plain arithmetic
@@ -400,7 +456,7 @@ template <int DK, int RT> struct Simt : Tile<4, DK> {
   static constexpr int SMEM = kWarps * (B::RING + QS + B::STAGES * 4);
 };
 
-template <int DK, int RT>
+template <int DK, int RT, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __grid_constant__ AttnParams a) {
   pdl_sync();
   using L = Simt<DK, RT>;
@@ -411,7 +467,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
 
   int64_t x0, x1;
   Place cur = {};
-  find_share(a, L::KT, x0, x1, cur);
+  if (CLUSTER) cluster_share(a, L::KT, x0, x1, cur);
+  else find_share(a, L::KT, x0, x1, cur);
   Pieces pieces;
   pieces.starts_here = cur.blk == 0;
   float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * (DK + 2);
@@ -420,6 +477,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
   const int key_l = lane % L::KT, part_l = lane / L::KT;
   float m[RT], l[RT], o[RT][L::VC];
   int len[RT], head[RT], q_row[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {      // a warp of a cluster may have no tile at all
+    m[r] = -INFINITY; l[r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < L::VC; ++c) o[r][c] = 0.f;
+  }
   bool fresh = true;
   int stage = 0;
   for (int64_t x = x0; x < x1; ++x) {
@@ -431,8 +494,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
       int row = 0, h = 0, row_keys = 0;
       if (lane < nr) {
         rows.place(a, cur, lane, row, h);
-        row_keys = row_len(a, row);
-        report_length(a, row);
+        row_keys = a.n_q == 1 ? cur.len : row_len(a, row);
       }
       const int64_t at = (int64_t)row * a.ldq + (int64_t)h * DK * 4;
       __syncwarp();
@@ -523,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
     }
     stage = (stage + 1) % L::STAGES;
     const bool item_ends = cur.blk + 1 == cur.nb;
-    if (item_ends || x + 1 == x1) {
+    if (!CLUSTER && (item_ends || x + 1 == x1)) {
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         if (r < nr) {
@@ -544,10 +606,26 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
       pieces.note(a, cur, item_ends);
       fresh = true;
     }
-    step(a, L::KT, cur);
+    if (CLUSTER) ++cur.blk;
+    else step(a, L::KT, cur);
   }
   cp_async_wait<0>();
-  finish_cta<float, DK, RT>(a, pieces.meta);
+  if (CLUSTER) {
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      float lt = part_l == 0 ? l[r] : 0.f;
+#pragma unroll
+      for (int of = 16; of > 0; of >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
+      float* at = reinterpret_cast<float*>(keys.ring) + r * (DK + 2);
+#pragma unroll
+      for (int c = 0; c < L::VC; ++c) at[lane * L::VC + c] = o[r][c];
+      if (lane == 0) { at[DK] = m[r]; at[DK + 1] = lt; }
+    }
+    finish_cluster<float, DK, RT>(a, cur, smem, L::RING);
+  } else {
+    finish_cta<float, DK, RT>(a, pieces.meta);
+  }
 }
 
 // ------------------------------------------------------------------ bfloat16: matrix instructions
@@ -565,21 +643,21 @@ template <int DK, int RT> struct Mma : Tile<2, DK> {
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 // c[0..1]: rows lane / 4, c[2..3]: rows lane / 4 + 8 (H16; otherwise those rows are zero and not kept)
 template <bool H16>
 __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if (H16) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   } else {
     float z0, z1;
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%5}, {%7,%8}, {%0,%1,%9,%9};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%5}, {%7,%8}, {%0,%1,%9,%9};"
                  : "+f"(c[0]), "+f"(c[1]), "=f"(z0), "=f"(z1) : "r"(a0), "r"(0), "r"(a2), "r"(b0), "r"(b1), "f"(0.f));
   }
 }
@@ -613,7 +691,7 @@ __device__ __noinline__ void values_by_key(const unsigned char* vt, const float*
     }
 }
 
-template <int DK, int RT>
+template <int DK, int RT, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_kernel(const __grid_constant__ AttnParams a) {
   pdl_sync();
   using L = Mma<DK, RT>;
@@ -626,7 +704,8 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
 
   int64_t x0, x1;
   Place cur = {};
-  find_share(a, L::KT, x0, x1, cur);
+  if (CLUSTER) cluster_share(a, L::KT, x0, x1, cur);
+  else find_share(a, L::KT, x0, x1, cur);
   Pieces pieces;
   pieces.starts_here = cur.blk == 0;
   float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * (DK + 2);
@@ -636,6 +715,12 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
   float m[NH], l[NH], o[NT][CN], far[NH];
   const float* bias[NH];
   int len[NH], min_len = 0, max_len = 0;      // keys this lane's rows see; over all rows
+#pragma unroll
+  for (int hf = 0; hf < NH; ++hf) { m[hf] = -INFINITY; l[hf] = 0.f; }      // a warp of a cluster may have no tile at all
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < CN; ++i) o[t][i] = 0.f;
   bool fresh = true;
   int stage = 0;
   for (int64_t x = x0; x < x1; ++x) {
@@ -647,13 +732,12 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
       for (int hf = 0; hf < NH; ++hf) {
         const int r = lane / 4 + 8 * hf;
         const bool valid = r < rows.n;
-        m[hf] = -INFINITY; l[hf] = 0.f; len[hf] = 0; far[hf] = 0.f; bias[hf] = nullptr;
+        m[hf] = -INFINITY; l[hf] = 0.f; len[hf] = 0; far[hf] = 0.f; bias[hf] = a.bias;
         const uint32_t* src = nullptr;
         if (valid) {
           int row, h;
           rows.place(a, cur, r, row, h);
-          len[hf] = row_len(a, row);
-          if (quad == 0) report_length(a, row);
+          len[hf] = a.n_q == 1 ? cur.len : row_len(a, row);      // one token: known from the walk
           min_len = min(min_len, len[hf]); max_len = max(max_len, len[hf]);
           src = reinterpret_cast<const uint32_t*>(a.q + (int64_t)row * a.ldq + h * (DK * 2)) + quad;
           if (a.bias != nullptr) { bias[hf] = a.bias + (int64_t)h * a.n_bias; far[hf] = bias[hf][0]; }
@@ -664,6 +748,8 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
           qf[ks][NH + hf] = valid ? src[ks * 8 + 4] : 0u;
         }
       }
+      if (a.n_q == 1) min_len = max_len = cur.len;
+      else
 #pragma unroll
       for (int of = 4; of < 32; of <<= 1) {
         min_len = min(min_len, __shfl_xor_sync(0xffffffffu, min_len, of));
@@ -680,6 +766,25 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
     const int j0 = cur.blk * L::KT;
     const uint32_t ok = vmask[stage];
     if (ok != 0) {
+      // bias of the tile, on its way while the scores are formed.  Behind the distance where it saturates it is one value
+      // per row.
+      const bool near = a.bias != nullptr && a.n_bias - min_len + j0 + L::KT - 1 > 0;
+      float add[NG * 2][CN];
+      if (near) {
+#pragma unroll
+        for (int hf = 0; hf < NH; ++hf) {
+          const int at = a.n_bias - len[hf] + j0 + quad * 2;
+#pragma unroll
+          for (int t = 0; t < NG * 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) add[t][2 * hf + i] = bias[hf][min(max(at + t * 8 + i, 0), a.n_bias - 1)];
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < NG * 2; ++t)
+#pragma unroll
+          for (int i = 0; i < CN; ++i) add[t][i] = far[i >> 1];
+      }
       const uint32_t kt = keys.ring_s + stage * 2 * L::BYTES, vt = kt + L::BYTES;
       float s[NG * 2][CN];
 #pragma unroll
@@ -697,8 +802,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
           mma16816<H16>(s[2 * g + 1], qf[ks][0], qf[ks][NH - 1], qf[ks][NH], qf[ks][2 * NH - 1], b[2], b[3]);
         }
       }
-      // scores: scale, bias, mask.  Behind the distance where the bias saturates it is one value per row.
-      const bool near = a.bias != nullptr && a.n_bias - min_len + j0 + L::KT - 1 > 0;
+      // scores: scale, bias, mask
       const bool all_seen = ok == (L::KT == 32 ? 0xffffffffu : (1u << L::KT) - 1u) && j0 + L::KT <= min_len;
       float top[NH];
 #pragma unroll
@@ -706,25 +810,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
 #pragma unroll
       for (int t = 0; t < NG * 2; ++t)
 #pragma unroll
-        for (int i = 0; i < CN; ++i) s[t][i] = fmaf(s[t][i], a.scale, near ? 0.f : far[i >> 1]);
-      if (near && all_seen && a.n_bias - max_len + j0 >= 0) {      // every distance of the tile has its entry
-#pragma unroll
-        for (int hf = 0; hf < NH; ++hf) {
-          if (bias[hf] != nullptr) {
-            const float* at = bias[hf] + (a.n_bias - len[hf] + j0 + quad * 2);
-#pragma unroll
-            for (int t = 0; t < NG * 2; ++t) { s[t][2 * hf] += at[t * 8]; s[t][2 * hf + 1] += at[t * 8 + 1]; }
-          }
-        }
-      } else if (near) {
-#pragma unroll
-        for (int t = 0; t < NG * 2; ++t)
-#pragma unroll
-          for (int i = 0; i < CN; ++i) {
-            const int hf = i >> 1, j = j0 + t * 8 + quad * 2 + (i & 1);
-            if (j < len[hf]) s[t][i] += bias[hf][max(a.n_bias - len[hf] + j, 0)];
-          }
-      }
+        for (int i = 0; i < CN; ++i) s[t][i] = fmaf(s[t][i], a.scale, add[t][i]);
       if (!all_seen) {
         const uint32_t mine = ok >> (quad * 2);
 #pragma unroll
@@ -811,7 +897,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
     }
     stage = (stage + 1) % L::STAGES;
     const bool item_ends = cur.blk + 1 == cur.nb;
-    if (item_ends || x + 1 == x1) {
+    if (!CLUSTER && (item_ends || x + 1 == x1)) {
       const Rows rows(a, cur, RT);
       const bool whole = pieces.whole(item_ends);
 #pragma unroll
@@ -842,10 +928,27 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
       pieces.note(a, cur, item_ends);
       fresh = true;
     }
-    step(a, L::KT, cur);
+    if (CLUSTER) ++cur.blk;
+    else step(a, L::KT, cur);
   }
   cp_async_wait<0>();
-  finish_cta<bf16, DK, RT>(a, pieces.meta);
+  if (CLUSTER) {
+    __syncwarp();
+#pragma unroll
+    for (int hf = 0; hf < NH; ++hf) {
+      float lt = l[hf];
+      lt += __shfl_xor_sync(0xffffffffu, lt, 1);
+      lt += __shfl_xor_sync(0xffffffffu, lt, 2);
+      float* at = reinterpret_cast<float*>(keys.ring) + (lane / 4 + 8 * hf) * (DK + 2);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        *reinterpret_cast<float2*>(at + t * 8 + quad * 2) = make_float2(o[t][2 * hf], o[t][2 * hf + 1]);
+      if (quad == 0) { at[DK] = m[hf]; at[DK + 1] = lt; }
+    }
+    finish_cluster<bf16, DK, RT>(a, cur, smem, L::RING);
+  } else {
+    finish_cta<bf16, DK, RT>(a, pieces.meta);
+  }
 }
 
 // Joins the pieces of the item that the boundary behind CTA blockIdx.x is the first to cut; one CTA per boundary and query
@@ -923,7 +1026,8 @@ __global__ void __launch_bounds__(128) paged_attn_join_kernel(const __grid_const
 using Kernel = void (*)(AttnParams);
 
 // CTAs that fill the GPU with this kernel, looked up once per device
-template <typename T, int DK, int RT>
+// CTAs that fill the GPU with this kernel, looked up (and its shared memory allowed) once per device
+template <typename T, int DK, int RT, bool CLUSTER>
 cudaError_t grid_of(Kernel kernel, int smem, int* ctas) {
   static std::atomic<int> known[64];
   int dev = 0;
@@ -945,28 +1049,58 @@ cudaError_t grid_of(Kernel kernel, int smem, int* ctas) {
   return cudaSuccess;
 }
 
+// A cluster per item when all clusters are resident at once and no warp gets more than four tiles, by the keys the page
+// table could name; 0: shares of the line
+int cluster_size(int64_t items, int64_t cap, int kt) {
+  const int64_t tiles = (cap + kt - 1) / kt;
+  int c = 1;
+  while (c < 8 && c * kWarps < tiles) c *= 2;
+  return items * c <= 2 * 148 && tiles <= 4 * c * kWarps ? c : 0;
+}
+
 template <typename T, int DK, int RT>
-cudaError_t run_attention(AttnParams& a, Kernel kernel, int smem, cudaStream_t st) {
+cudaError_t run_attention(AttnParams& a, Kernel line, Kernel clustered, int smem, cudaStream_t st) {
+  using L = Tile<sizeof(T), DK>;
   int ctas = 0;
-  a.runs = a.pool.page_size % Tile<sizeof(T), DK>::RUN == 0;
-  cudaError_t e = grid_of<T, DK, RT>(kernel, smem, &ctas);
-  if (e != cudaSuccess) return e;
+  a.runs = a.pool.page_size % L::RUN == 0;
   a.tiles = (a.n_q * a.m + RT - 1) / RT;
   a.rows = a.n_q * a.m < RT ? a.n_q * a.m : RT;
   a.by_m = FastDiv(a.m); a.by_tiles = FastDiv(a.tiles); a.by_items = FastDiv(a.G * a.tiles);
-  e = launch_pdl(kernel, dim3(ctas), dim3(kThreads), (size_t)smem, st, a);
+  const int64_t items = (int64_t)a.S * a.G * a.tiles;
+  a.cluster = cluster_size(items, a.cap, L::KT);
+  if (a.cluster > 0) {
+    cudaError_t e = grid_of<T, DK, RT, true>(clustered, smem, &ctas);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(items * a.cluster)); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = a.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, clustered, a);
+  }
+  cudaError_t e = grid_of<T, DK, RT, false>(line, smem, &ctas);
+  if (e != cudaSuccess) return e;
+  a.by_workers = FastDiv(ctas * kWarps);
+  e = launch_pdl(line, dim3(ctas), dim3(kThreads), (size_t)smem, st, a);
   if (e != cudaSuccess) return e;
   return launch_pdl(paged_attn_join_kernel<T, DK, RT>, dim3(ctas - 1, a.rows), dim3(128), 0, st, a, ctas);
 }
 // Rows of a tile: one row alone spares the float32 kernel seven eighths of its arithmetic; 8 rows half of the matrix
 // kernel's softmax
+template <int DK, int RT> cudaError_t run_simt(AttnParams& a, cudaStream_t st) {
+  return run_attention<float, DK, RT>(a, paged_attn_simt_kernel<DK, RT, false>, paged_attn_simt_kernel<DK, RT, true>, Simt<DK, RT>::SMEM, st);
+}
+template <int DK, int RT> cudaError_t run_mma(AttnParams& a, cudaStream_t st) {
+  return run_attention<bf16, DK, RT>(a, paged_attn_mma_kernel<DK, RT, false>, paged_attn_mma_kernel<DK, RT, true>, Mma<DK, RT>::SMEM, st);
+}
 template <int DK> cudaError_t run_f32(AttnParams& a, cudaStream_t st) {
-  if (a.n_q * a.m == 1) return run_attention<float, DK, 1>(a, paged_attn_simt_kernel<DK, 1>, Simt<DK, 1>::SMEM, st);
-  return run_attention<float, DK, 8>(a, paged_attn_simt_kernel<DK, 8>, Simt<DK, 8>::SMEM, st);
+  return a.n_q * a.m == 1 ? run_simt<DK, 1>(a, st) : run_simt<DK, 8>(a, st);
 }
 template <int DK> cudaError_t run_bf16(AttnParams& a, cudaStream_t st) {
-  if (a.n_q * a.m <= 8) return run_attention<bf16, DK, 8>(a, paged_attn_mma_kernel<DK, 8>, Mma<DK, 8>::SMEM, st);
-  return run_attention<bf16, DK, 16>(a, paged_attn_mma_kernel<DK, 16>, Mma<DK, 16>::SMEM, st);
+  return a.n_q * a.m <= 8 ? run_mma<DK, 8>(a, st) : run_mma<DK, 16>(a, st);
 }
 
 }  // namespace
