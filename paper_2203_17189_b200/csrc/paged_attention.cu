@@ -453,7 +453,8 @@ template <int DK, int RT> struct Simt : Tile<4, DK> {
   static constexpr int PARTS = 32 / B::KT, CL = B::CPR / PARTS;      // lanes per key, chunks per lane
   static constexpr int VC = DK / 32;                                 // output columns per lane
   static constexpr int QS = RT * DK * 4;                             // query rows of a warp's item
-  static constexpr int SMEM = kWarps * (B::RING + QS + B::STAGES * 4);
+  static constexpr int PS = RT > 1 ? B::KT * RT * 4 : 0;             // weights of a tile, [key][row]
+  static constexpr int SMEM = kWarps * (B::RING + QS + PS + B::STAGES * 4);
 };
 
 template <int DK, int RT, bool CLUSTER>
@@ -463,7 +464,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
   extern __shared__ __align__(128) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   float* qs = reinterpret_cast<float*>(smem + kWarps * L::RING + w * L::QS);
-  uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * (L::RING + L::QS)) + w * L::STAGES;
+  float* ps = reinterpret_cast<float*>(smem + kWarps * (L::RING + L::QS) + w * L::PS);
+  uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * (L::RING + L::QS + L::PS)) + w * L::STAGES;
 
   int64_t x0, x1;
   Place cur = {};
@@ -503,7 +505,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
       for (int i = 0; i < (RT * PER + 31) / 32; ++i) {
         const int idx = i * 32 + lane, r = idx / PER;
         const int64_t o = __shfl_sync(0xffffffffu, at, r & 31);
-        if (r < nr) reinterpret_cast<float4*>(qs)[idx] = *reinterpret_cast<const float4*>(a.q + o + (idx % PER) * 16);
+        if (r < RT) {      // rows beyond the tile's are zero: they see no key
+          const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+          reinterpret_cast<float4*>(qs)[idx] = r < nr ? *reinterpret_cast<const float4*>(a.q + o + (idx % PER) * 16) : none;
+        }
       }
       __syncwarp();
 #pragma unroll
@@ -536,49 +541,73 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
         const float4 k4 = *reinterpret_cast<const float4*>(kt + key_l * L::ROW + swz<L::CPR>(key_l, ch) * 16);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-          if (r < nr) {
-            const float4 q4 = *reinterpret_cast<const float4*>(qs + r * DK + ch * 4);
-            sc[r] = fmaf(q4.x, k4.x, sc[r]); sc[r] = fmaf(q4.y, k4.y, sc[r]);
-            sc[r] = fmaf(q4.z, k4.z, sc[r]); sc[r] = fmaf(q4.w, k4.w, sc[r]);
-          }
+          const float4 q4 = *reinterpret_cast<const float4*>(qs + r * DK + ch * 4);
+          sc[r] = fmaf(q4.x, k4.x, sc[r]); sc[r] = fmaf(q4.y, k4.y, sc[r]);
+          sc[r] = fmaf(q4.z, k4.z, sc[r]); sc[r] = fmaf(q4.w, k4.w, sc[r]);
         }
       }
+      bool all_see = true;      // every row sees every key of the tile that exists
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        if (r < nr) {
 #pragma unroll
-          for (int of = L::KT; of < 32; of <<= 1) sc[r] += __shfl_xor_sync(0xffffffffu, sc[r], of);
-          const bool seen = ((ok >> key_l) & 1) && j < len[r];
-          const float s = seen ? fmaf(sc[r], a.scale, add[r]) : -INFINITY;
-          float mx = s;
+        for (int of = L::KT; of < 32; of <<= 1) sc[r] += __shfl_xor_sync(0xffffffffu, sc[r], of);
+        const bool seen = ((ok >> key_l) & 1) && j < len[r];
+        all_see &= r >= nr || min(j0 + L::KT, cur.len) <= len[r];
+        const float s = seen ? fmaf(sc[r], a.scale, add[r]) : -INFINITY;
+        float mx = s;
 #pragma unroll
-          for (int of = 16; of > 0; of >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, of));
-          mx = fmaxf(m[r], mx);
-          const float ref = mx == -INFINITY ? 0.f : mx;
-          const float corr = ex2((m[r] - ref) * kLog2e);
-          const float p = ex2((s - ref) * kLog2e);
-          m[r] = mx;
-          l[r] = l[r] * corr + p;
-          sc[r] = p;
+        for (int of = 16; of > 0; of >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, of));
+        mx = fmaxf(m[r], mx);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        const float corr = ex2((m[r] - ref) * kLog2e);
+        sc[r] = ex2((s - ref) * kLog2e);
+        m[r] = mx;
+        l[r] = l[r] * corr + sc[r];
 #pragma unroll
-          for (int c = 0; c < L::VC; ++c) o[r][c] *= corr;
-        } else {
-          sc[r] = 0.f;
-        }
+        for (int c = 0; c < L::VC; ++c) o[r][c] *= corr;
       }
-#pragma unroll 8
-      for (int kk = 0; kk < L::KT; ++kk) {
-        struct alignas(L::VC * 4) Cols { float v[L::VC]; };
+      if (RT > 1) {      // the weights in shared memory: two loads give a key's weights of eight rows
+        __syncwarp();
+        if (part_l == 0) {
+#pragma unroll
+          for (int r = 0; r < RT; ++r) ps[key_l * RT + r] = sc[r];
+        }
+        __syncwarp();
+      }
+      struct alignas(L::VC * 4) Cols { float v[L::VC]; };
+      auto values = [&](int kk) {
         const int byte = lane * L::VC * 4;
-        const Cols vf = *reinterpret_cast<const Cols*>(vt + kk * L::ROW + swz<L::CPR>(kk, byte >> 4) * 16 + (byte & 15));
+        return *reinterpret_cast<const Cols*>(vt + kk * L::ROW + swz<L::CPR>(kk, byte >> 4) * 16 + (byte & 15));
+      };
+      if (RT == 1) {
+#pragma unroll 8
+        for (int kk = 0; kk < L::KT; ++kk) {
+          const Cols vf = values(kk);
+          const float p = __shfl_sync(0xffffffffu, sc[0], kk);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          if (r < nr) {
-            const float p = __shfl_sync(0xffffffffu, sc[r], kk);
-            // a key this row does not see has weight 0 and may hold anything: its value must not enter
-            const bool seen = RT == 1 || j0 + kk < len[r];
+          for (int c = 0; c < L::VC; ++c) o[0][c] = fmaf(p, vf.v[c], o[0][c]);
+        }
+      } else if (all_see) {
+#pragma unroll 8
+        for (int kk = 0; kk < L::KT; ++kk) {
+          const Cols vf = values(kk);
 #pragma unroll
-            for (int c = 0; c < L::VC; ++c) o[r][c] = seen ? fmaf(p, vf.v[c], o[r][c]) : o[r][c];
+          for (int r = 0; r < RT; ++r) {
+            const float p = ps[kk * RT + r];
+#pragma unroll
+            for (int c = 0; c < L::VC; ++c) o[r][c] = fmaf(p, vf.v[c], o[r][c]);
+          }
+        }
+      } else {
+        // a key that a row does not see has weight 0 there and may hold anything: its value must not enter
+#pragma unroll 1
+        for (int kk = 0; kk < L::KT; ++kk) {
+          const Cols vf = values(kk);
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            const float p = ps[kk * RT + r];
+#pragma unroll
+            for (int c = 0; c < L::VC; ++c) o[r][c] = j0 + kk < len[r] ? fmaf(p, vf.v[c], o[r][c]) : o[r][c];
           }
         }
       }
@@ -1088,8 +1117,7 @@ cudaError_t run_attention(AttnParams& a, Kernel line, Kernel clustered, int smem
   if (e != cudaSuccess) return e;
   return launch_pdl(paged_attn_join_kernel<T, DK, RT>, dim3(ctas - 1, a.rows), dim3(128), 0, st, a, ctas);
 }
-// Rows of a tile: one row alone spares the float32 kernel seven eighths of its arithmetic; 8 rows half of the matrix
-// kernel's softmax
+// Rows of a tile: the float32 kernel's arithmetic goes with them (1, 4, 8), the matrix kernel's softmax by halves (8, 16)
 template <int DK, int RT> cudaError_t run_simt(AttnParams& a, cudaStream_t st) {
   return run_attention<float, DK, RT>(a, paged_attn_simt_kernel<DK, RT, false>, paged_attn_simt_kernel<DK, RT, true>, Simt<DK, RT>::SMEM, st);
 }
@@ -1097,7 +1125,8 @@ template <int DK, int RT> cudaError_t run_mma(AttnParams& a, cudaStream_t st) {
   return run_attention<bf16, DK, RT>(a, paged_attn_mma_kernel<DK, RT, false>, paged_attn_mma_kernel<DK, RT, true>, Mma<DK, RT>::SMEM, st);
 }
 template <int DK> cudaError_t run_f32(AttnParams& a, cudaStream_t st) {
-  return a.n_q * a.m == 1 ? run_simt<DK, 1>(a, st) : run_simt<DK, 8>(a, st);
+  const int rows = a.n_q * a.m;
+  return rows == 1 ? run_simt<DK, 1>(a, st) : rows <= 4 ? run_simt<DK, 4>(a, st) : run_simt<DK, 8>(a, st);
 }
 template <int DK> cudaError_t run_bf16(AttnParams& a, cudaStream_t st) {
   return a.n_q * a.m <= 8 ? run_mma<DK, 8>(a, st) : run_mma<DK, 16>(a, st);
