@@ -54,6 +54,7 @@ struct AttnParams {
   float* part;           // [ctas][2][rows][d + 2]: the same of a CTA
   int4* meta;            // [ctas]: which pieces those are, see below
   int cluster;           // CTAs per item when every item has a cluster of its own
+  int extra;             // tiles that an item counts beside its own (find_share)
   int rows;              // query rows of a slot: min(RT, n_q m)
   int* status;
 };
@@ -95,16 +96,20 @@ __device__ __forceinline__ void step(const AttnParams& a, int bk, Place& p) {
   if (++p.s < a.S) { p.len = seq_len(a, p.s); p.nb = blocks_of(p.len, bk); }
 }
 
-// This warp's share [x0, x1) of the line and the place of x0.  Called by all threads.
+// This warp's share, tiles [x0, x1) of the line, and the place of x0.  Called by all threads.
+// An item counts as its tiles and a.extra more, for what its start and end cost (measured: shares of equal tiles alone ended
+// 15 us apart on 128 short sequences with a bias): the line that is cut is made of such units, the extra ones in front of
+// an item's tiles, and a cut inside them falls on the item's first tile.
 __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1, Place& p) {
+  constexpr int kEnds = kWarps + 1;      // where the warps' shares begin, and the next CTA's
   __shared__ int64_t sums[kWarps];
-  __shared__ int64_t found_prefix[kWarps];
-  __shared__ int found_s[kWarps];
+  __shared__ int64_t found_prefix[kEnds];
+  __shared__ int found_s[kEnds];
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-  int64_t mine = 0;      // tiles per item of this thread's sequences
+  int64_t mine = 0;      // units per item of this thread's sequences
   int first = 0;
   for (int s = tid; s < a.S; s += kThreads) {
-    const int n = blocks_of(seq_len(a, s), bk);
+    const int n = blocks_of(seq_len(a, s), bk) + a.extra;
     if (s == tid) first = n;
     mine += n;
     if (blockIdx.x == 0)
@@ -117,28 +122,22 @@ __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1
   int64_t total = 0;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) total += sums[i];
-  const int64_t items = (int64_t)a.G * a.tiles, n_w = (int64_t)gridDim.x * kWarps;
-  total *= items;
-  // share c: [c q + min(c, r), ...) with total = q n_w + r, so fewer tiles than warps leave the last warps without work.
-  // Lane i looks at the CTA's i-th share; a division of 64 bits takes as long as a memory access and is left to huge totals.
-  const bool small = total < (1ll << 31);
-  const int64_t q = small ? (int64_t)a.by_workers.div((uint32_t)total) : total / n_w, rest = total - q * n_w;
+  const int64_t items = (int64_t)a.G * a.tiles, n_w = (int64_t)gridDim.x * kWarps, line = total * items;
+  // Lane i looks at the CTA's i-th cut: cut c of n_w at c q + min(c, r), line = q n_w + r.  A division of 64 bits takes as
+  // long as a memory access and is left to huge totals.
+  const bool small = line < (1ll << 31);
+  const int64_t q = small ? (int64_t)a.by_workers.div((uint32_t)line) : line / n_w, rest = line - q * n_w;
   const int64_t c = (int64_t)blockIdx.x * kWarps + min(lane, kWarps);
-  const int64_t begin = c * q + min(c, rest);
-  const int64_t mine_at = small ? (int64_t)a.by_items.div((uint32_t)begin) : begin / items;
-  x0 = __shfl_sync(0xffffffffu, begin, w);
-  x1 = __shfl_sync(0xffffffffu, begin, w + 1);
-  int64_t at[kWarps];      // where the warps' shares begin, in tiles of one item per sequence (-1: no share)
+  const int64_t cut = c * q + min(c, rest);
+  const int64_t my_at = small ? (int64_t)a.by_items.div((uint32_t)cut) : cut / items;
+  int64_t at[kEnds];      // in units of one item per sequence
 #pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    const int64_t v = __shfl_sync(0xffffffffu, mine_at, i);
-    at[i] = __shfl_sync(0xffffffffu, begin, i) < __shfl_sync(0xffffffffu, begin, i + 1) ? v : -1;
-  }
-  // the sequence whose tiles hold x0: prefix(s) <= x0 / items < prefix(s + 1)
+  for (int i = 0; i < kEnds; ++i) at[i] = __shfl_sync(0xffffffffu, my_at, i);
+  // the sequences that hold the cuts: prefix(s) <= at < prefix(s + 1)
   int64_t base = 0;
-  for (int s0 = 0; s0 < a.S; s0 += kThreads) {
+  for (int s0 = 0; s0 < a.S && base <= at[kWarps]; s0 += kThreads) {
     const int s = s0 + tid;
-    const int n = s >= a.S ? 0 : (s0 == 0 ? first : blocks_of(seq_len(a, s), bk));
+    const int n = s >= a.S ? 0 : (s0 == 0 ? first : blocks_of(seq_len(a, s), bk) + a.extra);
     int64_t inc = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -155,18 +154,28 @@ __device__ void find_share(const AttnParams& a, int bk, int64_t& x0, int64_t& x1
       base += sums[i];
     }
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i)
+    for (int i = 0; i < kEnds; ++i)
       if (at[i] >= before && at[i] < before + n) { found_s[i] = s; found_prefix[i] = before; }
-    if (at[kWarps - 1] >= 0 ? at[kWarps - 1] < base : at[0] < base && at[1] < base && at[2] < base) break;
   }
   __syncthreads();
-  if (x0 == x1) return;
-  p.s = found_s[w];
-  p.len = seq_len(a, p.s);
-  p.nb = blocks_of(p.len, bk);
-  const int64_t in = x0 - found_prefix[w] * items;
-  p.k = small ? (int)((uint32_t)in / (uint32_t)p.nb) : (int)(in / p.nb);
-  p.blk = (int)(in - (int64_t)p.k * p.nb);
+  // lane i: place of cut i, and the tiles in front of it
+  Place m = {};
+  int64_t tiles = (total - (int64_t)a.extra * a.S) * items;      // a cut at the line's end
+  const int e = min(lane, kWarps);
+  if (cut < line) {
+    m.s = found_s[e];
+    m.len = seq_len(a, m.s);
+    m.nb = blocks_of(m.len, bk);
+    const int64_t in = cut - found_prefix[e] * items;
+    const int per = m.nb + a.extra;
+    m.k = small ? (int)((uint32_t)in / (uint32_t)per) : (int)(in / per);
+    m.blk = max((int)(in - (int64_t)m.k * per) - a.extra, 0);
+    tiles = (found_prefix[e] - (int64_t)a.extra * m.s) * items + (int64_t)m.k * m.nb + m.blk;
+  }
+  x0 = __shfl_sync(0xffffffffu, tiles, w);
+  x1 = __shfl_sync(0xffffffffu, tiles, w + 1);
+  p.s = __shfl_sync(0xffffffffu, m.s, w); p.k = __shfl_sync(0xffffffffu, m.k, w); p.blk = __shfl_sync(0xffffffffu, m.blk, w);
+  p.nb = __shfl_sync(0xffffffffu, m.nb, w); p.len = __shfl_sync(0xffffffffu, m.len, w);
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {
@@ -741,9 +750,9 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
   KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, lane);
 
   uint32_t qf[KS][2 * NH];               // A operand: columns 16 ks + 2 quad (+ 8), rows lane / 4 (+ 8)
-  float m[NH], l[NH], o[NT][CN], far[NH];
+  float m[NH], l[NH], o[NT][CN], far[NH], add[NG * 2][CN] = {}, next[NG * 2][CN] = {};
   const float* bias[NH];
-  int len[NH], min_len = 0, max_len = 0;      // keys this lane's rows see; over all rows
+  int len[NH], min_len = 0;      // keys this lane's rows see; the fewest of any row
 #pragma unroll
   for (int hf = 0; hf < NH; ++hf) { m[hf] = -INFINITY; l[hf] = 0.f; }      // a warp of a cluster may have no tile at all
 #pragma unroll
@@ -753,67 +762,64 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
   bool fresh = true;
   int stage = 0;
   for (int64_t x = x0; x < x1; ++x) {
-    if (fresh) {
-      fresh = false;
-      const Rows rows(a, cur, RT);
-      min_len = 0x7fffffff; max_len = 0;
-#pragma unroll
-      for (int hf = 0; hf < NH; ++hf) {
-        const int r = lane / 4 + 8 * hf;
-        const bool valid = r < rows.n;
-        m[hf] = -INFINITY; l[hf] = 0.f; len[hf] = 0; far[hf] = 0.f; bias[hf] = a.bias;
-        const uint32_t* src = nullptr;
-        if (valid) {
-          int row, h;
-          rows.place(a, cur, r, row, h);
-          len[hf] = a.n_q == 1 ? cur.len : row_len(a, row);      // one token: known from the walk
-          min_len = min(min_len, len[hf]); max_len = max(max_len, len[hf]);
-          src = reinterpret_cast<const uint32_t*>(a.q + (int64_t)row * a.ldq + h * (DK * 2)) + quad;
-          if (a.bias != nullptr) { bias[hf] = a.bias + (int64_t)h * a.n_bias; far[hf] = bias[hf][0]; }
-        }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          qf[ks][hf] = valid ? src[ks * 8] : 0u;
-          qf[ks][NH + hf] = valid ? src[ks * 8 + 4] : 0u;
-        }
-      }
-      if (a.n_q == 1) min_len = max_len = cur.len;
-      else
-#pragma unroll
-      for (int of = 4; of < 32; of <<= 1) {
-        min_len = min(min_len, __shfl_xor_sync(0xffffffffu, min_len, of));
-        max_len = max(max_len, __shfl_xor_sync(0xffffffffu, max_len, of));
-      }
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < CN; ++i) o[t][i] = 0.f;
-    }
-    cp_async_wait<L::STAGES - 2>();
-    __syncwarp();
-    keys.issue((stage + L::STAGES - 1) % L::STAGES);
-    const int j0 = cur.blk * L::KT;
-    const uint32_t ok = vmask[stage];
-    if (ok != 0) {
-      // bias of the tile, on its way while the scores are formed.  Behind the distance where it saturates it is one value
-      // per row.
-      const bool near = a.bias != nullptr && a.n_bias - min_len + j0 + L::KT - 1 > 0;
-      float add[NG * 2][CN];
-      if (near) {
+    // What is added to the scores of a tile from key j0 on.  Behind the distance where the bias saturates that is one value
+    // per row.  Loads of an SM come back in the order they went out, so a tile's bias is fetched in front of the copies
+    // that follow the tile's own: fetched when it is needed it cost 0.85 us a tile.
+    auto load_add = [&](int j0, float (&to)[NG * 2][CN]) {
+      if (a.n_bias - min_len + j0 + L::KT - 1 > 0) {
 #pragma unroll
         for (int hf = 0; hf < NH; ++hf) {
           const int at = a.n_bias - len[hf] + j0 + quad * 2;
 #pragma unroll
           for (int t = 0; t < NG * 2; ++t)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) add[t][2 * hf + i] = bias[hf][min(max(at + t * 8 + i, 0), a.n_bias - 1)];
+            for (int i = 0; i < 2; ++i) to[t][2 * hf + i] = bias[hf][min(max(at + t * 8 + i, 0), a.n_bias - 1)];
         }
       } else {
 #pragma unroll
         for (int t = 0; t < NG * 2; ++t)
 #pragma unroll
-          for (int i = 0; i < CN; ++i) add[t][i] = far[i >> 1];
+          for (int i = 0; i < CN; ++i) to[t][i] = far[i >> 1];
       }
+    };
+    if (fresh) {
+      fresh = false;
+      const Rows rows(a, cur, RT);
+      min_len = 0x7fffffff;
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf) {
+        const int r = lane / 4 + 8 * hf;
+        const bool valid = r < rows.n;      // rows beyond the tile's repeat its first one and are not kept
+        int row, h;
+        rows.place(a, cur, valid ? r : 0, row, h);
+        m[hf] = -INFINITY; l[hf] = 0.f; far[hf] = 0.f; bias[hf] = a.bias;
+        len[hf] = a.n_q == 1 ? cur.len : row_len(a, row);      // one token: known from the walk
+        min_len = min(min_len, len[hf]);
+        if (a.bias != nullptr) { bias[hf] = a.bias + (int64_t)h * a.n_bias; far[hf] = bias[hf][0]; }
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (int64_t)row * a.ldq + h * (DK * 2)) + quad;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          qf[ks][hf] = src[ks * 8];
+          qf[ks][NH + hf] = src[ks * 8 + 4];
+        }
+      }
+      if (a.n_q > 1) {
+#pragma unroll
+        for (int of = 4; of < 32; of <<= 1) min_len = min(min_len, __shfl_xor_sync(0xffffffffu, min_len, of));
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < CN; ++i) o[t][i] = 0.f;
+      if (a.bias != nullptr) load_add(cur.blk * L::KT, add);
+    }
+    const int j0 = cur.blk * L::KT;
+    if (a.bias != nullptr && cur.blk + 1 < cur.nb) load_add(j0 + L::KT, next);
+    cp_async_wait<L::STAGES - 2>();
+    __syncwarp();
+    keys.issue((stage + L::STAGES - 1) % L::STAGES);
+    const uint32_t ok = vmask[stage];
+    if (ok != 0) {
       const uint32_t kt = keys.ring_s + stage * 2 * L::BYTES, vt = kt + L::BYTES;
       float s[NG * 2][CN];
 #pragma unroll
@@ -925,6 +931,12 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
       }
     }
     stage = (stage + 1) % L::STAGES;
+    if (a.bias != nullptr) {
+#pragma unroll
+      for (int t = 0; t < NG * 2; ++t)
+#pragma unroll
+        for (int i = 0; i < CN; ++i) add[t][i] = next[t][i];
+    }
     const bool item_ends = cur.blk + 1 == cur.nb;
     if (!CLUSTER && (item_ends || x + 1 == x1)) {
       const Rows rows(a, cur, RT);
@@ -991,8 +1003,8 @@ __global__ void __launch_bounds__(128) paged_attn_join_kernel(const __grid_const
   const Place p = item_place(a, item);
   const Rows rows(a, p, RT);
   if (r >= rows.n) return;
-  // pieces: slot 1 of c0, then slot 0 of the CTAs behind it up to the one where the item ends (CTAs without work
-  // lie behind all others)
+  // pieces: slot 1 of c0, then slot 0 of the CTAs behind it up to the one where the item ends (a CTA without work lies
+  // between items, never inside one)
   __shared__ int s_last;
   if (tid == 0) s_last = ctas - 1;
   __syncthreads();
@@ -1113,6 +1125,7 @@ cudaError_t run_attention(AttnParams& a, Kernel line, Kernel clustered, int smem
   cudaError_t e = grid_of<T, DK, RT, false>(line, smem, &ctas);
   if (e != cudaSuccess) return e;
   a.by_workers = FastDiv(ctas * kWarps);
+  a.extra = a.bias != nullptr ? 2 : 1;
   e = launch_pdl(line, dim3(ctas), dim3(kThreads), (size_t)smem, st, a);
   if (e != cudaSuccess) return e;
   return launch_pdl(paged_attn_join_kernel<T, DK, RT>, dim3(ctas - 1, a.rows), dim3(128), 0, st, a, ctas);

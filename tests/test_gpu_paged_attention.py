@@ -35,6 +35,13 @@ def workspace(r, n_q, h, g, d):
     return ws
 
 
+def widened(table, page):
+    """The same pages in a table that could name 2^18 keys: the call may no longer assume a short cache."""
+    wide = torch.full((table.shape[0], max(table.shape[1], (1 << 18) // page)), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    return wide
+
+
 def attend(q, kp, vp, table, lens, scale, n_q, bias, ws=None):
     out = torch.full_like(q, float("nan"), memory_format=torch.contiguous_format)
     lse = torch.full(q.shape[:2], float("nan"), device=DEV)
@@ -56,6 +63,7 @@ def check(q, kp, vp, table, lens, scale, n_q, bias):
     return out, lse
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("seq_lens,n_q,h,g,d,page,n_bias,layout", [
     ([1], 1, 1, 1, 32, 16, 0, "slots"),
@@ -72,10 +80,10 @@ def check(q, kp, vp, table, lens, scale, n_q, bias):
     ([150], 64, 2, 2, 64, 16, 20, "slots"),
     ([70, 333], 1, 40, 2, 64, 16, 0, "heads"),
     ([50, 61], 3, 64, 2, 128, 128, 500, "slots")])
-def test_matches_plain_form(dtype, seq_lens, n_q, h, g, d, page, n_bias, layout):
+def test_matches_plain_form(dtype, seq_lens, n_q, h, g, d, page, n_bias, layout, wide):
     rng = np.random.default_rng(len(seq_lens) * 100 + h)
     q, kp, vp, table, lens, bias = build(rng, seq_lens, n_q, h, g, d, page, dtype, layout, n_bias)
-    check(q, kp, vp, table, lens, d ** -0.5, n_q, bias)
+    check(q, kp, vp, widened(table, page) if wide else table, lens, d ** -0.5, n_q, bias)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -88,21 +96,25 @@ def test_many_sequences_of_every_length(dtype):
     check(q, kp, vp, table, lens, 0.2, 1, bias)
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_lengths_of_a_sequences_rows_in_no_order(dtype):
+def test_lengths_of_a_sequences_rows_in_no_order(dtype, wide):
     """Rows that share a sequence may see any number of its keys, none included."""
     rng = np.random.default_rng(12)
     q, kp, vp, table, _, bias = build(rng, [300, 300, 40], 6, 4, 2, 64, 16, dtype, n_bias=17)
+    table = widened(table, 16) if wide else table
     lens = [300, 0, 1, 150, 64, 299, 0, 0, 0, 300, 17, 16, 0, -3, 40, 39, 1, 2]
     check(q, kp, vp, table, lens, 0.125, 6, bias)
 
 
 @pytest.mark.parametrize("dtype,n_q,h,g", [(F32, 4, 4, 4), (BF16, 4, 4, 4), (BF16, 4, 8, 2), (BF16, 8, 8, 2)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_keys_a_row_does_not_see_may_hold_anything(dtype, n_q, h, g, bad):
+@pytest.mark.parametrize("wide", [False, True])
+def test_keys_a_row_does_not_see_may_hold_anything(dtype, n_q, h, g, bad, wide):
     """The later tokens of a draft hold NaN or infinities: the earlier rows do not notice."""
     rng = np.random.default_rng(13)
     q, kp, vp, table, lens, bias = build(rng, [100, 67], n_q, h, g, 64, 16, dtype, n_bias=128)
+    table = widened(table, 16) if wide else table
     want, want_lse = attend(q, kp, vp, table, lens, 0.1, n_q, bias)
     for s, n in enumerate([100, 67]):
         pg, sl = SR.slots_of(table, s, n, 16)
@@ -123,11 +135,13 @@ def test_keys_a_row_does_not_see_may_hold_anything(dtype, n_q, h, g, bad):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("low", [-float("inf"), torch.finfo(F32).min])
-def test_bias_that_masks(dtype, low):
+@pytest.mark.parametrize("wide", [False, True])
+def test_bias_that_masks(dtype, low, wide):
     """A bias of the type's lowest value or of -infinity: on the far keys it removes them; on all keys the lowest value
     leaves a uniform mean, -infinity an empty row."""
     rng = np.random.default_rng(14)
     q, kp, vp, table, lens, bias = build(rng, [200, 33, 5], 1, 2, 2, 64, 16, dtype, n_bias=64)
+    table = widened(table, 16) if wide else table
     bias[0, :40] = low      # head 0 sees the nearest 24 keys
     bias[1] = low           # head 1 sees nothing, or everything alike
     out, lse = attend(q, kp, vp, table, lens, 0.1, 1, bias)
@@ -148,11 +162,13 @@ def test_bias_that_masks(dtype, low):
             assert torch.isfinite(lse[r, 1])
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_sharp_and_large_scores(dtype):
+def test_sharp_and_large_scores(dtype, wide):
     """Scores of several hundred: the maximum moves often, the rest underflows to nothing."""
     rng = np.random.default_rng(15)
     q, kp, vp, table, lens, bias = build(rng, [400, 129], 1, 4, 2, 128, 16, dtype, spread=30.0)
+    table = widened(table, 16) if wide else table
     check(q, kp, vp, table, lens, 1.0, 1, None)
 
 
@@ -188,9 +204,12 @@ def test_cache_beyond_four_gigabytes():
     check(q, kp, vp, table, [150], 0.09, 1, None)
 
 
-def test_bad_pages_and_lengths_are_reported():
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("wide", [False, True])
+def test_bad_pages_and_lengths_are_reported(wide, dtype):
     rng = np.random.default_rng(18)
-    q, kp, vp, table, lens, _ = build(rng, [64, 64], 1, 2, 2, 64, 16, BF16)
+    q, kp, vp, table, lens, _ = build(rng, [64, 64], 1, 2, 2, 64, 16, dtype)
+    table = widened(table, 16) if wide else table
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
     Bd.t5_kernel_status_word(status)
     try:
@@ -206,10 +225,17 @@ def test_bad_pages_and_lengths_are_reported():
             k, v = kp[pg].reshape(-1, 2, 64).double(), vp[pg].reshape(-1, 2, 64).double()
             w = torch.softmax(torch.einsum("nhd,hd->hn", k, q[r].double()) * 0.1, -1)
             ref = torch.einsum("hn,nhd->hd", w, v)
-            assert (out[r].double() - ref).abs().max() <= (2.0 ** -8 + 2.0 ** -12) * v.abs().max()
+            assert (out[r].double() - ref).abs().max() <= (SR.HALF[dtype] + 2.0 ** -12) * v.abs().max()
         status.zero_()
-        out, _ = attend(q, kp, vp, good, [64, 1000], 0.1, 1, None)
-        assert status.item() == 203 and torch.equal(out, want)
+        if not wide:      # a length beyond what the table can name is cut to that
+            out, _ = attend(q, kp, vp, good, [64, 1000], 0.1, 1, None)
+            assert status.item() == 203 and torch.equal(out, want)
+        else:             # here it reaches into entries that name no page
+            out, _ = attend(q, kp, vp, good, [64, 1000], 0.1, 1, None)
+            assert status.item() == 202 and torch.isfinite(out).all()
+            status.zero_()
+            attend(q, kp, vp, good, [64, (1 << 18) + 1], 0.1, 1, None)
+            assert status.item() in (202, 203)
     finally:
         Bd.t5_kernel_status_word(None)
 
