@@ -198,6 +198,26 @@ T5_API int t5_decode_step(t5_handle* h, const void* d_params, void* d_cache, int
                           int32_t Tmax, int32_t t, const int32_t* d_tokens, void* d_logits, void* d_workspace,
                           int64_t workspace_bytes, void* stream);
 
+/* One decoding step of the model over paged caches: S sequences at positions of their own, n_new (1 .. 64) tokens each
+ * (1: the usual step; more: a prompt taken in pieces, or a draft to be verified), the decoder's self-attention through
+ * t5_paged_kv_append and t5_paged_attention.  The result at position t of a sequence equals row t of t5_decode_logits.
+ *  - d_pool: t5_decode_pool_bytes(n_pages, page_size) bytes, not initialised: per decoder layer a pool of keys and a pool
+ *    of values, [n_pages, page_size, heads, d_kv] each.  One page table serves all layers.
+ *  - d_tokens, d_positions [S * n_new]: decoder INPUT tokens (0 at position 0) and their positions; a negative position
+ *    is an unused slot (its token must be a valid id, its logits are undefined).  A token sees its sequence's positions
+ *    up to its own, those of this call included; a position may be written again (a refused draft), what lies behind the
+ *    last written position is never read.
+ *  - encoder-decoder: d_cross_cache is a cache filled by t5_decode_begin(B = S, Te, Tmax = 1); else NULL with Te = 0.
+ *  - d_logits [S * n_new, vocab] in the configured dtype.
+ * A token that finds no page leaves a code for t5_device_status(d_workspace). */
+T5_API int t5_decode_pool_bytes(const t5_handle* h, int32_t n_pages, int32_t page_size, int64_t* bytes);
+T5_API int t5_decode_step_paged_workspace_bytes(const t5_handle* h, int32_t S, int32_t n_new, int64_t* bytes);
+T5_API int t5_decode_step_paged(t5_handle* h, const void* d_params, void* d_pool, int64_t pool_bytes, int32_t n_pages,
+                                int32_t page_size, const int32_t* d_page_table, int32_t max_pages, int64_t ld_table,
+                                int32_t S, int32_t n_new, const int32_t* d_tokens, const int32_t* d_positions,
+                                const void* d_cross_cache, int64_t cross_cache_bytes, int32_t Te, void* d_logits,
+                                void* d_workspace, int64_t workspace_bytes, void* stream);
+
 /* Data-parallel training ("XLA GSPMD partitioning" section: data parallelism
  * with replicated parameters; the partitioner there inserts the gradient
  * all-reduce, here the caller does, overlapped with the backward pass).
@@ -223,7 +243,8 @@ T5_API int t5_set_grad_hook(t5_handle* h, t5_grad_ready_fn fn, void* user);
 /* Reads back the status word the kernels of the last call on this workspace
  * left behind (their waits on TMA/tensor-core barriers are bounded; one that
  * runs out records a code instead of spinning).  SYNCHRONISES the stream.
- * Returns T5_OK or T5_ERR_DEVICE_TIMEOUT. */
+ * Returns T5_OK, T5_ERR_DEVICE_TIMEOUT, or T5_ERR_SHAPE for a token that found
+ * no place in a paged cache (codes 201 - 203 below). */
 T5_API int t5_device_status(t5_handle* h, const void* d_workspace, void* stream);
 
 /* Measurement aids (no counterpart in the paper).  With profiling enabled every

@@ -56,7 +56,7 @@ EXPORTS = ["t5_create", "t5_destroy", "t5_last_error", "t5_param_count", "t5_par
            "t5_gemm", "t5_attention", "t5_attention_backward_noalloc",
            "t5_attention_ds_scratch_bytes", "t5_attention_backward_onepass",
            "t5_kernel_status_word", "t5_selftest_bounded_wait", "t5_set_grad_hook",
-           "t5_paged_kv_append", "t5_paged_attention_workspace_bytes", "t5_paged_attention", "t5_verify_draft"]
+           "t5_decode_pool_bytes", "t5_decode_step_paged_workspace_bytes", "t5_decode_step_paged", "t5_paged_kv_append", "t5_paged_attention_workspace_bytes", "t5_paged_attention", "t5_verify_draft"]
 
 _lib = None
 
@@ -91,6 +91,9 @@ def lib():
         L.t5_decode_step_workspace_bytes.argtypes = [vp, i32, C.POINTER(i64)]
         L.t5_decode_begin.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, i64, vp]
         L.t5_decode_step.argtypes = [vp, vp, vp, i64, i32, i32, i32, i32, vp, vp, vp, i64, vp]
+        L.t5_decode_pool_bytes.argtypes = [vp, i32, i32, C.POINTER(i64)]
+        L.t5_decode_step_paged_workspace_bytes.argtypes = [vp, i32, i32, C.POINTER(i64)]
+        L.t5_decode_step_paged.argtypes = [vp, vp, vp, i64, i32, i32, vp, i32, i64, i32, i32, vp, vp, vp, i64, i32, vp, vp, i64, vp]
         L.t5_encode.argtypes = [vp, vp, C.POINTER(t5_batch), vp, vp, i64, vp]
         L.t5_decode_logits.argtypes = [vp, vp, C.POINTER(t5_batch), vp, vp, vp, i64, vp]
         L.t5_device_status.argtypes = [vp, vp, vp]
@@ -256,6 +259,33 @@ class Handle:
         _check(lib().t5_decode_step(self._h, _ptr(params), _ptr(cache), cache.numel() * cache.element_size(), B, Te, Tmax,
                                     t, _ptr(tokens), _ptr(logits), _ptr(workspace),
                                     workspace.numel() * workspace.element_size(), _stream()), self._h)
+
+    def t5_decode_pool_bytes(self, n_pages, page_size):
+        n = C.c_int64()
+        _check(lib().t5_decode_pool_bytes(self._h, n_pages, page_size, C.byref(n)), self._h)
+        return n.value
+
+    def t5_decode_step_paged_workspace_bytes(self, S, n_new):
+        n = C.c_int64()
+        _check(lib().t5_decode_step_paged_workspace_bytes(self._h, S, n_new, C.byref(n)), self._h)
+        return n.value
+
+    def t5_decode_step_paged(self, params, pool, n_pages, page_size, page_table, tokens, positions, logits, workspace,
+                             cross_cache=None, Te=0):
+        """page_table [S, max_pages], tokens / positions [S, n_new] int32, logits [S, n_new, vocab]."""
+        S, n_new = tokens.shape
+        if (page_table.shape[0] != S or positions.shape != tokens.shape or tuple(logits.shape) != (S, n_new, self.cfg.vocab)
+                or logits.dtype != self.torch_dtype or not all(t.is_contiguous() for t in (tokens, positions, logits))
+                or any(t.dtype != torch.int32 for t in (page_table, tokens, positions)) or page_table.stride(1) != 1):
+            raise T5Error(-8, "want int32 page_table [S, pages], contiguous int32 tokens and positions [S, n_new] and logits "
+                              "[S, n_new, vocab] of the model's type")
+        ld = page_table.stride(0) if S > 1 else page_table.shape[1]
+        _check(lib().t5_decode_step_paged(self._h, _ptr(params), _ptr(pool), pool.numel() * pool.element_size(), n_pages,
+                                          page_size, _ptr(page_table), page_table.shape[1], ld, S, n_new, _ptr(tokens),
+                                          _ptr(positions), _ptr(cross_cache),
+                                          0 if cross_cache is None else cross_cache.numel() * cross_cache.element_size(), Te,
+                                          _ptr(logits), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                          _stream()), self._h)
 
     def t5_encode(self, params, batch, enc_out, workspace):
         b = self._batch(batch)

@@ -188,6 +188,7 @@ cudaError_t launch_prep(const int* enc_tok, const int* enc_seg, const int* dec_t
                         const int* dec_prefix, int B, int Te, int Td, int* enc_code, int* dec_code, int* dec_in,
                         float* dec_w, int* W_int, float* W_f, cudaStream_t st);
 cudaError_t launch_pad_codes(const int* tok, int* code, int n, cudaStream_t st);      // code = tok != 0
+cudaError_t launch_lens_of_positions(const int* pos, int* lens, int n, cudaStream_t st);
 cudaError_t launch_set_column(int* p, int ld, int col, int rows, int value, cudaStream_t st);
 // X[t] = E[tok[t]] (float32); with g != NULL also XG[t] = X[t] * g (dtype T) and ssq[t] = sum X[t]^2
 cudaError_t launch_embed_gather(int dtype, const void* E, const int* tok, float* X, const void* g, void* XG,

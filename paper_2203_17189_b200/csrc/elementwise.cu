@@ -82,6 +82,11 @@ __global__ void set_column_kernel(int* __restrict__ p, int ld, int col, int rows
   int r = blockIdx.x * blockDim.x + threadIdx.x;
   if (r < rows) p[(int64_t)r * ld + col] = value;
 }
+// keys a token at position p sees: p + 1; a negative position (unused slot) sees none
+__global__ void lens_of_positions_kernel(const int* __restrict__ pos, int* __restrict__ lens, int n) {
+  int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < n) lens[i] = pos[i] < 0 ? 0 : (pos[i] < 0x7fffffff ? pos[i] + 1 : pos[i]);
+}
 __global__ void w_to_float_kernel(const int* W_int, float* W_f) { *W_f = (float)(*W_int); }
 
 // ------------------------------------------------------------------ embedding
@@ -633,6 +638,12 @@ cudaError_t launch_pad_codes(const int* tok, int* code, int n, cudaStream_t st) 
 cudaError_t launch_set_column(int* p, int ld, int col, int rows, int value, cudaStream_t st) {
   if (rows == 0) return cudaSuccess;
   set_column_kernel<<<blocks_for(rows, 128), 128, 0, st>>>(p, ld, col, rows, value);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_lens_of_positions(const int* pos, int* lens, int n, cudaStream_t st) {
+  if (n == 0) return cudaSuccess;
+  lens_of_positions_kernel<<<blocks_for(n, 128), 128, 0, st>>>(pos, lens, n);
   return cudaGetLastError();
 }
 

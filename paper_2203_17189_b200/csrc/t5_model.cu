@@ -2,6 +2,7 @@
 // plan, the forward/backward launch schedule of the T5.1.1 step, and the C ABI.
 #include "../../include/t5_b200.h"
 #include "common.cuh"
+#include "paged.cuh"
 
 #include <math.h>
 #include <stdarg.h>
@@ -927,6 +928,78 @@ void attn_step(Ctx& cx, const AttnP& p, const AttnWs& a, float* x_out, const Nex
   proj_fwd_residual(cx, a.ctx, I, p.o, B, d, I, x_out, a.x, &nn, "o proj (step)");
 }
 
+// The same over a paged cache: n_new positions per sequence, each sequence at its own; k, v of the new rows enter the
+// layer's pools on the way.
+struct PagedStep {
+  PagedPool pool;            // of the layer at hand
+  const int *positions, *lens;
+  const float* bias;
+  int n_bias, n_new;
+  void* attn_ws;
+};
+void attn_step_paged(Ctx& cx, const AttnP& p, const AttnWs& a, float* x_out, const NextNorm& nn, const PagedStep& ps) {
+  const t5_config& c = cx.h->cfg;
+  const int d = c.d_model, I = c.n_heads * c.d_kv, rows = cx.B * ps.n_new;
+  proj_fwd(cx, a.xg, d, p.q, rows, 3 * I, d, a.q, 3 * I, 1.f, row_norm(cx, a.ssq), "qkv proj (paged step)");
+  PagedAppendArgs pa;
+  memset(&pa, 0, sizeof pa);
+  pa.dtype = c.dtype; pa.n_tokens = rows; pa.n_kv_heads = c.n_heads; pa.d_kv = c.d_kv;
+  pa.k = eoff(cx.h, a.q, I); pa.v = eoff(cx.h, a.q, 2 * I); pa.ldk = pa.ldv = 3 * I;
+  pa.pos = ps.positions; pa.tokens_per_seq = ps.n_new; pa.pool = ps.pool; pa.n_seqs = cx.B; pa.status = cx.w->status;
+  CKL(CAT_ATTN_FWD, 1, launch_paged_append(pa, cx.st), "append to the paged cache");
+  PagedAttnArgs ta;
+  memset(&ta, 0, sizeof ta);
+  ta.dtype = c.dtype; ta.n_rows = rows; ta.n_q = ps.n_new; ta.H = ta.Hkv = c.n_heads; ta.d_kv = c.d_kv;
+  ta.q = a.q; ta.ldq = 3 * I; ta.out = a.ctx; ta.ldo = I; ta.lens = ps.lens; ta.bias = ps.bias; ta.n_bias = ps.n_bias;
+  ta.scale = c.attn_scale; ta.pool = ps.pool; ta.workspace = ps.attn_ws; ta.status = cx.w->status;
+  CKL(CAT_ATTN_FWD, 2, launch_paged_attention(ta, cx.st), "paged attention");
+  proj_fwd_residual(cx, a.ctx, I, p.o, rows, d, I, x_out, a.x, &nn, "o proj (paged step)");
+}
+// Cross-attention of n_new positions per sequence over the keys / values that t5_decode_begin projected
+void cross_step(Ctx& cx, const AttnP& p, const AttnWs& a, float* x_out, const NextNorm& nn, const void* kv, int Te,
+                const int* code_k, const int* ones, int n_new) {
+  const t5_config& c = cx.h->cfg;
+  const int d = c.d_model, I = c.n_heads * c.d_kv, rows = cx.B * n_new;
+  proj_fwd(cx, a.xg, d, p.q, rows, I, d, a.q, I, 1.f, row_norm(cx, a.ssq), "q proj (paged step)");
+  AttnArgs ta{};
+  ta.Q = a.q; ta.ldq = I; ta.K = kv; ta.V = eoff(cx.h, kv, I); ta.ldk = ta.ldv = 2 * I;
+  ta.O = a.ctx; ta.ldo = I; ta.lse = a.lse; ta.O32 = a.ctx32; ta.ldo32 = I;
+  ta.B = cx.B; ta.H = c.n_heads; ta.Tq = n_new; ta.Tk = Te; ta.dk = c.d_kv;
+  ta.code_q = ones; ta.code_k = code_k; ta.scale = c.attn_scale; ta.packed = 1;
+  if (c.dtype == DT_BF16 && !(c.flags & 2) && attn_tc_supported(ta))
+    CKL(CAT_ATTN_FWD, 1, attn_fwd_tc(ta, cx.w->status, cx.st), "cross attention (paged step, tcgen05)");
+  else
+    CKL(CAT_ATTN_FWD, 1, attn_fwd_simt(c.dtype, ta, cx.st), "cross attention (paged step)");
+  proj_fwd_residual(cx, a.ctx, I, p.o, rows, d, I, x_out, a.x, &nn, "o proj (paged step)");
+}
+// Workspace of a paged step: that of the decoder on n_new positions per row, and behind it the step's own arrays
+struct PagedWs {
+  int *lens, *ones;
+  float* bias;
+  void* attn;
+  int n_bias;
+  int64_t bytes;
+};
+void plan_paged_step(const t5_handle* h, int S, int n_new, char* base, Workspace* w, PagedWs* p) {
+  const t5_config& c = h->cfg;
+  plan_workspace(h, S, 0, n_new, base, w);
+  int64_t cur = w->bytes;
+  auto take = [&](int64_t bytes) -> void* {
+    const int64_t at = cur;
+    cur += (bytes + 255) / 256 * 256;
+    return base ? (void*)(base + at) : nullptr;
+  };
+  p->n_bias = saturation_distance(h->spec_dec) + 1;
+  p->lens = (int*)take((int64_t)S * n_new * 4);
+  p->ones = (int*)take((int64_t)S * n_new * 4);
+  p->bias = (float*)take((int64_t)c.n_heads * p->n_bias * 4);
+  p->attn = take(paged_attention_workspace(S * n_new, n_new, c.n_heads, c.n_heads, c.d_kv));
+  p->bytes = cur;
+}
+int64_t layer_pool_bytes(const t5_handle* h, int64_t n_pages, int64_t page_size) {      // of keys or of values
+  return n_pages * page_size * h->cfg.n_heads * h->cfg.d_kv * (int64_t)esize(h);
+}
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // Common argument checks; fills cx and lays out the workspace.
@@ -1285,6 +1358,96 @@ int t5_decode_step_workspace_bytes(const t5_handle* h, int32_t B, int64_t* bytes
   return T5_OK;
 }
 
+int t5_decode_pool_bytes(const t5_handle* h, int32_t n_pages, int32_t page_size, int64_t* bytes) {
+  if (!h || !bytes) return T5_ERR_NULL;
+  if (n_pages < 1 || page_size < 1) return T5_ERR_ARG;
+  *bytes = 2 * h->cfg.n_dec_layers * layer_pool_bytes(h, n_pages, page_size);
+  return T5_OK;
+}
+
+int t5_decode_step_paged_workspace_bytes(const t5_handle* h, int32_t S, int32_t n_new, int64_t* bytes) {
+  if (!h || !bytes) return T5_ERR_NULL;
+  if (S < 1 || S > h->cfg.max_batch || n_new < 1 || n_new > 64) return T5_ERR_ARG;
+  Workspace w;
+  PagedWs p;
+  plan_paged_step(h, S, n_new, nullptr, &w, &p);
+  *bytes = p.bytes;
+  return T5_OK;
+}
+
+int t5_decode_step_paged(t5_handle* h, const void* d_params, void* d_pool, int64_t pool_bytes, int32_t n_pages,
+                         int32_t page_size, const int32_t* d_page_table, int32_t max_pages, int64_t ld_table, int32_t S,
+                         int32_t n_new, const int32_t* d_tokens, const int32_t* d_positions, const void* d_cross_cache,
+                         int64_t cross_cache_bytes, int32_t Te, void* d_logits, void* d_workspace, int64_t workspace_bytes,
+                         void* stream) {
+  if (!h) return T5_ERR_NULL;
+  const t5_config& c = h->cfg;
+  const bool encdec = c.arch == 0;
+  if (!d_params || !d_pool || !d_page_table || !d_tokens || !d_positions || !d_logits || !d_workspace ||
+      (encdec && !d_cross_cache))
+    return fail(h, T5_ERR_NULL, "null pointer");
+  if (S < 1 || S > c.max_batch || n_new < 1 || n_new > 64 || n_pages < 1 || page_size < 1 || max_pages < 1 ||
+      ld_table < max_pages || (encdec && (Te < 1 || Te > c.max_enc_len)))
+    return fail(h, T5_ERR_SHAPE, "decode_step_paged: %d sequences, %d new tokens, %d pages of %d, %d pages a sequence, %d encoder positions",
+                S, n_new, n_pages, page_size, max_pages, Te);
+  if (!aligned16(d_params) || !aligned16(d_pool) || !aligned16(d_logits) || !aligned16(d_workspace) || !aligned16(d_cross_cache))
+    return fail(h, T5_ERR_ALIGN, "params / pool / logits / workspace / cross cache not 16-byte aligned");
+  const int64_t per_pool = layer_pool_bytes(h, n_pages, page_size);
+  if (pool_bytes / 2 / c.n_dec_layers < per_pool)
+    return fail(h, T5_ERR_WORKSPACE, "pool of %lld bytes given, %lld needed", (long long)pool_bytes,
+                (long long)(2 * c.n_dec_layers * per_pool));
+  DecodeCache k;
+  if (encdec) {
+    plan_cache(h, S, Te, 1, (char*)const_cast<void*>(d_cross_cache), &k);
+    if (k.bytes > cross_cache_bytes)
+      return fail(h, T5_ERR_WORKSPACE, "cross cache of %lld bytes given, %lld needed", (long long)cross_cache_bytes, (long long)k.bytes);
+  }
+  Workspace w;
+  PagedWs p;
+  plan_paged_step(h, S, n_new, (char*)d_workspace, &w, &p);
+  if (p.bytes > workspace_bytes)
+    return fail(h, T5_ERR_WORKSPACE, "workspace of %lld bytes given, %lld needed", (long long)workspace_bytes, (long long)p.bytes);
+  PagedStep ps;
+  const int64_t slot = (int64_t)c.n_heads * c.d_kv;
+  const int rc = paged_pool_args((int)esize(h), c.n_heads, c.d_kv, d_pool, d_pool, n_pages, page_size, slot * page_size, slot,
+                                 c.d_kv, d_page_table, S, max_pages, ld_table, &ps.pool);
+  if (rc != T5_OK) return fail(h, rc, "decode_step_paged: %d pages of %d positions per sequence", max_pages, page_size);
+  ps.positions = d_positions; ps.lens = p.lens; ps.bias = p.bias; ps.n_bias = p.n_bias; ps.n_new = n_new; ps.attn_ws = p.attn;
+  Ctx cx{};
+  cx.h = h; cx.params = d_params; cx.st = (cudaStream_t)stream; cx.w = &w; cx.B = S; cx.Te = 0; cx.Td = n_new;
+  cx.err = cudaSuccess; cx.where = "";
+  const int L = c.n_dec_layers, d = c.d_model, rows = S * n_new;
+  CK(cudaMemsetAsync(w.status, 0, 4, cx.st), "memset status");
+  CK(cudaMemsetAsync(w.sk_flags, 0, (int64_t)kSkSlices * kSkSliceInts * 4, cx.st), "memset stream-K flags");
+  CK(cudaMemsetAsync(w.ssq_all, 0, w.ssq_floats * 4, cx.st), "memset row statistics");
+  CKL(CAT_MISC, 1, launch_lens_of_positions(d_positions, p.lens, rows, cx.st), "lengths (paged step)");
+  if (encdec) CK(launch_set_column(p.ones, 1, 0, rows, 1, cx.st), "ones");
+  // entry n_bias - 1 - distance: one key ahead of n_bias queries
+  CKL(CAT_MISC, 1, launch_relbias_expand(c.dtype, h->spec_dec, pptr(h, d_params, h->dec_relbias), c.n_heads, p.n_bias, 1, p.bias,
+                                         cx.st),
+      "relbias_expand (paged step)");
+  float* x0 = w.dec_self[0].x;
+  NextNorm n0 = dec_norm_at(cx, 0, 0);
+  CKL(CAT_EMBED, 1, launch_embed_gather(c.dtype, pptr(h, d_params, h->token_embed), d_tokens, x0, pptr(h, d_params, n0.g_off),
+                                        n0.xg, n0.ssq, rows, d, cx.st),
+      "embed (paged step)");
+  for (int l = 0; l < L; ++l) {
+    ps.pool.k = (char*)d_pool + 2 * l * per_pool;
+    ps.pool.v = ps.pool.k + per_pool;
+    float* after_self = encdec ? w.dec_cross[l].x : w.dec_ffn[l].x;
+    attn_step_paged(cx, h->dec[l].self, w.dec_self[l], after_self, dec_norm_at(cx, l, encdec ? 1 : 2), ps);
+    if (encdec)
+      cross_step(cx, h->dec[l].cross, w.dec_cross[l], w.dec_ffn[l].x, dec_norm_at(cx, l, 2), k.cross_kv[l], Te, k.enc_code, p.ones,
+                 n_new);
+    float* x_next = l + 1 < L ? w.dec_self[l + 1].x : w.dec_x_final;
+    ffn_forward(cx, h->dec[l].ffn, w.dec_ffn[l], x_next, dec_norm_at(cx, l + 1, 0), rows);
+  }
+  const int64_t head = h->lm_head >= 0 ? h->lm_head : h->token_embed;
+  proj_fwd(cx, w.dec_xg_f, d, head, rows, c.vocab, d, d_logits, c.vocab, c.logit_scale, row_norm(cx, w.dec_ssq_f),
+           "logits (paged step)");
+  return end_call(h, cx);
+}
+
 int t5_device_status(t5_handle* h, const void* d_workspace, void* stream) {
   if (!h || !d_workspace) return T5_ERR_NULL;
   int status = 0;
@@ -1292,6 +1455,8 @@ int t5_device_status(t5_handle* h, const void* d_workspace, void* stream) {
   cudaError_t e = cudaMemcpyAsync(&status, d_workspace, sizeof(int), cudaMemcpyDeviceToHost, st);
   if (e == cudaSuccess) e = cudaStreamSynchronize(st);
   if (e != cudaSuccess) return fail(h, T5_ERR_CUDA, "device_status: %s", cudaGetErrorString(e));
+  if (status >= PAGED_BAD_APPEND && status <= PAGED_BAD_LENGTH)
+    return fail(h, T5_ERR_SHAPE, "a token found no place in the paged cache (code %d: position, page or length out of range)", status);
   if (status != 0) return fail(h, T5_ERR_DEVICE_TIMEOUT, "a bounded device-side wait ran out (code %d)", status);
   return T5_OK;
 }
