@@ -667,14 +667,17 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
 }
 
 // ------------------------------------------------------------------ bfloat16: matrix instructions
-// S = Q K^T and O += P V as m16n8k16 products (float32 sums) whose 16 rows are query rows: heads that share the kv head,
-// and the new tokens of the sequence.  A single row fills a sixteenth of them, and the tensor pipe is idle all the same:
-// what counts is that a key costs few instructions.  tcgen05 needs 64 or 128 rows and a trip through tensor memory per
-// tile; here neither operand nor result leaves the registers between load and use.
-// RT = 8 leaves the lower half of the rows out of the softmax and of the registers.
-// The weights go into the second product as a sum of two bfloat16 parts (error 2^-17 instead of 2^-9 for 8 more matrix
-// instructions per 16 keys, on a pipe that has the room), so the output is the float32 result rounded once.
-template <int DK, int RT> struct Mma : Tile<2, DK> {
+// m16n8k16 products with float32 sums.  Up to 8 query rows (heads that share the kv head, new tokens of the sequence) are
+// the 8 columns of S^T = K Q^T and O^T += V^T P^T, 16 keys or 16 columns the 16 rows (paged_attn_rows8_kernel): 24
+// instructions per 16 keys of 128 columns.  With more rows they are the 16 rows of S = Q K^T and O += P V, 16 at a time
+// (paged_attn_rows16_kernel): 48; 8 rows as half of 16 took 305 instead of 292 us on 6 x 29 heads of 64 columns over 47,600
+// keys.  A single row fills an eighth of the instructions, which costs nothing more.  tcgen05 needs 64 or 128 rows and a
+// trip through tensor memory per tile; here neither operand nor result leaves the registers between load and use.  What
+// bounds these kernels beside memory is the two warps that a scheduler has (registers and rings allow no more): about 430
+// instructions per 8 KB at five cycles each.
+// The weights go into the second product as a sum of two bfloat16 parts (error 2^-17 instead of 2^-9), so the output is the
+// float32 result rounded once; without the second part the calls above take 0 - 5 % less.
+template <int DK> struct Mma : Tile<2, DK> {
   using B = Tile<2, DK>;
   static constexpr int SMEM = kWarps * (B::RING + B::STAGES * 4);
 };
@@ -687,17 +690,16 @@ __device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
-// c[0..1]: rows lane / 4, c[2..3]: rows lane / 4 + 8 (H16; otherwise those rows are zero and not kept)
-template <bool H16>
-__device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  if (H16) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  } else {
-    float z0, z1;
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%5}, {%7,%8}, {%0,%1,%9,%9};"
-                 : "+f"(c[0]), "+f"(c[1]), "=f"(z0), "=f"(z1) : "r"(a0), "r"(0), "r"(a2), "r"(b0), "r"(b1), "f"(0.f));
-  }
+// c += a b: c[0..1] row lane / 4, c[2..3] row lane / 4 + 8, columns 2 (lane % 4) + 0, 1
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 8 x 8 transpose of pairs: in, lane holds row lane / 4, columns 2 (lane % 4) + 0, 1
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 // two floats as bfloat16 parts: hi = round(x), lo = round(x - hi)
 __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
@@ -711,31 +713,55 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t&
 __device__ __forceinline__ bool not_finite(uint32_t two) {      // either bfloat16 has an exponent of all ones
   return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
 }
-// O += P V of one tile without a product that a row does not see: s, o as in the kernel, rows see the first n0 / n1 keys
-template <int DK, int RT>
-__device__ __noinline__ void values_by_key(const unsigned char* vt, const float* s, float* o, int n0, int n1) {
-  using L = Mma<DK, RT>;
-  constexpr int CN = RT / 4;
+// O += P V of one tile without a product that a row does not see: s [2 tiles of 8 keys per 16][4], o [DK / 8][4] as in the
+// kernel of 16 rows; rows lane / 4 (+ 8) see the first n0 / n1 keys
+template <int DK>
+__device__ __noinline__ void values_by_key16(const unsigned char* vt, const float* s, float* o, int n0, int n1) {
+  using L = Mma<DK>;
   const int lane = threadIdx.x & 31, quad = lane & 3;
   for (int kk = 0; kk < L::KT; ++kk)
-    for (int hf = 0; hf < RT / 8; ++hf) {
-      const float p = __shfl_sync(0xffffffffu, s[(kk / 8) * CN + 2 * hf + (kk & 1)], (lane & ~3) | ((kk & 7) >> 1));
+    for (int hf = 0; hf < 2; ++hf) {
+      const float p = __shfl_sync(0xffffffffu, s[(kk / 8) * 4 + 2 * hf + (kk & 1)], (lane & ~3) | ((kk & 7) >> 1));
       if (kk < (hf ? n1 : n0))
         for (int t = 0; t < DK / 8; ++t) {
           const uint32_t u = *reinterpret_cast<const uint32_t*>(vt + kk * L::ROW + swz<L::CPR>(kk, t) * 16 + quad * 4);
-          o[t * CN + 2 * hf] = fmaf(p, __uint_as_float(u << 16), o[t * CN + 2 * hf]);
-          o[t * CN + 2 * hf + 1] = fmaf(p, __uint_as_float(u & 0xffff0000u), o[t * CN + 2 * hf + 1]);
+          o[t * 4 + 2 * hf] = fmaf(p, __uint_as_float(u << 16), o[t * 4 + 2 * hf]);
+          o[t * 4 + 2 * hf + 1] = fmaf(p, __uint_as_float(u & 0xffff0000u), o[t * 4 + 2 * hf + 1]);
         }
     }
 }
+// The same for the kernel of 8 rows: s [16 keys][4], o [DK / 16][4]; rows 2 (lane % 4) + 0, 1 see the first n0 / n1 keys
+template <int DK>
+__device__ __noinline__ void values_by_key8(const unsigned char* vt, const float* s, float* o, int n0, int n1) {
+  using L = Mma<DK>;
+  const int lane = threadIdx.x & 31, quad = lane & 3;
+  for (int kk = 0; kk < L::KT; ++kk)
+    for (int j = 0; j < 2; ++j) {
+      const float p = __shfl_sync(0xffffffffu, s[(kk / 16) * 4 + ((kk >> 3) & 1) * 2 + j], (kk & 7) * 4 + quad);
+      if (kk < (j ? n1 : n0))
+        for (int t = 0; t < DK / 8; ++t) {      // column 8 t + lane / 4
+          const bf16 v = *reinterpret_cast<const bf16*>(vt + kk * L::ROW + swz<L::CPR>(kk, t) * 16 + (lane >> 2) * 2);
+          o[(t / 2) * 4 + (t & 1) * 2 + j] = fmaf(p, to_f(v), o[(t / 2) * 4 + (t & 1) * 2 + j]);
+        }
+    }
+}
+template <int DK, int N>      // whether a tile of values holds one that is not finite
+__device__ __forceinline__ bool tile_not_finite(const unsigned char* vt, int lane) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < N / 512; ++i) {
+    const uint4 u = *reinterpret_cast<const uint4*>(vt + (i * 32 + lane) * 16);
+    bad |= not_finite(u.x) | not_finite(u.y) | not_finite(u.z) | not_finite(u.w);
+  }
+  return __any_sync(0xffffffffu, bad);
+}
 
-template <int DK, int RT, bool CLUSTER>
-__global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_kernel(const __grid_constant__ AttnParams a) {
+template <int DK, bool CLUSTER>
+__global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_rows8_kernel(const __grid_constant__ AttnParams a) {
   pdl_sync();
-  using L = Mma<DK, RT>;
-  constexpr bool H16 = RT == 16;
-  constexpr int NH = RT / 8;             // row halves: this lane's rows are lane / 4 (+ 8)
-  constexpr int KS = DK / 16, NG = L::KT / 16, NT = DK / 8, CN = 2 * NH;
+  using L = Mma<DK>;
+  constexpr int RT = 8;
+  constexpr int KS = DK / 16, NG = L::KT / 16, NT = DK / 16;
   extern __shared__ __align__(128) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, quad = lane & 3;
   uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * L::RING) + w * L::STAGES;
@@ -749,7 +775,256 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
   float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * (DK + 2);
   KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, lane);
 
-  uint32_t qf[KS][2 * NH];               // A operand: columns 16 ks + 2 quad (+ 8), rows lane / 4 (+ 8)
+  uint32_t qf[KS][2];                    // B operand: columns 16 ks + 2 quad (+ 8) of row lane / 4
+  // scores of this lane: keys lane / 4 + 8 (i / 2) of each 16, rows 2 quad + i % 2; outputs: columns 16 t + lane / 4 +
+  // 8 (i / 2), the same rows
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[NT][4] = {}, far[2], add[NG][4] = {}, next[NG][4] = {};
+  const float* bias[2];
+  int len[2], min_len = 0;      // keys this lane's rows see; the fewest of any row
+  bool fresh = true;
+  int stage = 0;
+  for (int64_t x = x0; x < x1; ++x) {
+    // What is added to the scores of a tile from key j0 on.  Behind the distance where the bias saturates that is one value
+    // per row.  Loads of an SM come back in the order they went out, so a tile's bias is fetched in front of the copies
+    // that follow the tile's own: fetched when it is needed it cost 0.85 us a tile.
+    auto load_add = [&](int j0, float (&to)[NG][4]) {
+      if (a.n_bias - min_len + j0 + L::KT - 1 > 0) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int at = a.n_bias - len[j] + j0 + (lane >> 2);
+#pragma unroll
+          for (int g = 0; g < NG * 2; ++g) to[g / 2][(g & 1) * 2 + j] = bias[j][min(max(at + g * 8, 0), a.n_bias - 1)];
+        }
+      } else {
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) to[g][i] = far[i & 1];
+      }
+    };
+    if (fresh) {
+      fresh = false;
+      const Rows rows(a, cur, RT);
+      min_len = 0x7fffffff;
+      int row, h;      // rows beyond the tile's repeat its first one and are not kept
+      rows.place(a, cur, (lane >> 2) < rows.n ? lane >> 2 : 0, row, h);
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (int64_t)row * a.ldq + h * (DK * 2)) + quad;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qf[ks][0] = src[ks * 8];
+        qf[ks][1] = src[ks * 8 + 4];
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        rows.place(a, cur, quad * 2 + j < rows.n ? quad * 2 + j : 0, row, h);
+        m[j] = -INFINITY; l[j] = 0.f; far[j] = 0.f; bias[j] = a.bias;
+        len[j] = a.n_q == 1 ? cur.len : row_len(a, row);      // one token: known from the walk
+        min_len = min(min_len, len[j]);
+        if (a.bias != nullptr) { bias[j] = a.bias + (int64_t)h * a.n_bias; far[j] = bias[j][0]; }
+      }
+      if (a.n_q > 1) {
+        min_len = min(min_len, __shfl_xor_sync(0xffffffffu, min_len, 1));
+        min_len = min(min_len, __shfl_xor_sync(0xffffffffu, min_len, 2));
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[t][i] = 0.f;
+      if (a.bias != nullptr) load_add(cur.blk * L::KT, add);
+    }
+    const int j0 = cur.blk * L::KT;
+    if (a.bias != nullptr && cur.blk + 1 < cur.nb) load_add(j0 + L::KT, next);
+    cp_async_wait<L::STAGES - 2>();
+    __syncwarp();
+    keys.issue((stage + L::STAGES - 1) % L::STAGES);
+    const uint32_t ok = vmask[stage];
+    if (ok != 0) {
+      const uint32_t kt = keys.ring_s + stage * 2 * L::BYTES, vt = kt + L::BYTES;
+      float s[NG][4];
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[g][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          uint32_t b[4];
+          const int row = g * 16 + (lane & 15);
+          ldsm4(kt + row * L::ROW + swz<L::CPR>(row, 2 * ks + (lane >> 4)) * 16, b);
+          mma16816(s[g], b, qf[ks][0], qf[ks][1]);
+        }
+      }
+      // scores: scale, bias, mask
+      const bool all_seen = ok == (L::KT == 32 ? 0xffffffffu : (1u << L::KT) - 1u) && j0 + L::KT <= min_len;
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[g][i] = fmaf(s[g][i], a.scale, add[g][i]);
+      if (!all_seen) {
+        const uint32_t mine = ok >> (lane >> 2);
+#pragma unroll
+        for (int g = 0; g < NG * 2; ++g)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            if (!((mine >> (g * 8)) & 1) || j0 + g * 8 + (lane >> 2) >= len[j]) s[g / 2][(g & 1) * 2 + j] = -INFINITY;
+      }
+      float top[2] = {m[0], m[1]}, ref[2];
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[i & 1] = fmaxf(top[i & 1], s[g][i]);
+      bool moved = false;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int of = 4; of < 32; of <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], of));
+        ref[j] = top[j] == -INFINITY ? 0.f : top[j];
+        moved |= top[j] != m[j];
+      }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float corr = ex2((m[j] - ref[j]) * kLog2e);
+          l[j] *= corr;
+          m[j] = top[j];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) { o[t][j] *= corr; o[t][2 + j] *= corr; }
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[g][i] = ex2((s[g][i] - ref[i & 1]) * kLog2e);      // differences first: a bias of the lowest float stays finite
+          l[i & 1] += s[g][i];
+        }
+      // Keys that one row sees and another does not have weight 0 there, and 0 x NaN would spoil the row: if such a tile
+      // holds a value that is not finite, it is taken key by key.
+      const unsigned char* values = keys.ring + stage * 2 * L::BYTES + L::BYTES;
+      const bool plain = min_len < min(j0 + L::KT, cur.len) && tile_not_finite<DK, L::BYTES>(values, lane);
+      if (!plain) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          uint32_t hi[2], lo[2];      // weights of keys 0 - 7 and 8 - 15: from [key][row] to [row][key]
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            split2(s[g][2 * i], s[g][2 * i + 1], hi[i], lo[i]);
+            hi[i] = transpose8(hi[i]);
+            lo[i] = transpose8(lo[i]);
+          }
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            uint32_t b[4];
+            const int row = g * 16 + (lane & 7) + (lane >> 4) * 8;
+            ldsm4_t(vt + row * L::ROW + swz<L::CPR>(row, 2 * t + ((lane >> 3) & 1)) * 16, b);
+            mma16816(o[t], b, hi[0], hi[1]);
+            mma16816(o[t], b, lo[0], lo[1]);
+          }
+        }
+      } else {
+        // copies, so that the rare call below does not push the registers of the others into memory
+        float sc[NG * 4], oc[NT * 4];
+#pragma unroll
+        for (int i = 0; i < NG * 4; ++i) sc[i] = s[i / 4][i % 4];
+#pragma unroll
+        for (int i = 0; i < NT * 4; ++i) oc[i] = o[i / 4][i % 4];
+        values_by_key8<DK>(values, sc, oc, len[0] - j0, len[1] - j0);
+#pragma unroll
+        for (int i = 0; i < NT * 4; ++i) o[i / 4][i % 4] = oc[i];
+      }
+    }
+    stage = (stage + 1) % L::STAGES;
+    if (a.bias != nullptr) {
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) add[g][i] = next[g][i];
+    }
+    const bool item_ends = cur.blk + 1 == cur.nb;
+    if (!CLUSTER && (item_ends || x + 1 == x1)) {
+      const Rows rows(a, cur, RT);
+      const bool whole = pieces.whole(item_ends);
+      float lt[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        lt[j] = l[j];
+#pragma unroll
+        for (int of = 4; of < 32; of <<= 1) lt[j] += __shfl_xor_sync(0xffffffffu, lt[j], of);
+      }
+      if (whole) {
+        int row, h;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          if (lane < 4 && quad * 2 + j < rows.n) {
+            rows.place(a, cur, quad * 2 + j, row, h);
+            write_lse(a, row, h, m[j], lt[j]);
+          }
+        const float inv0 = lt[0] == 0.f ? 0.f : 1.f / lt[0], inv1 = lt[1] == 0.f ? 0.f : 1.f / lt[1];
+        const bool mine = (lane >> 2) < rows.n;
+        rows.place(a, cur, mine ? lane >> 2 : 0, row, h);
+        bf16* at = out_row<bf16, DK>(a, row, h) + quad * 2;
+#pragma unroll
+        for (int t = 0; t < NT * 2; ++t) {      // columns 8 t ...: from [column][row] to [row][column]
+          const __nv_bfloat162 v = __floats2bfloat162_rn(o[t / 2][(t & 1) * 2] * inv0, o[t / 2][(t & 1) * 2 + 1] * inv1);
+          const uint32_t u = transpose8(*reinterpret_cast<const uint32_t*>(&v));
+          if (mine) *reinterpret_cast<uint32_t*>(at + t * 8) = u;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          if (quad * 2 + j < rows.n) {
+            float* at = part + (pieces.slot() * a.rows + quad * 2 + j) * (DK + 2);
+#pragma unroll
+            for (int t = 0; t < NT * 2; ++t) at[t * 8 + (lane >> 2)] = o[t / 2][(t & 1) * 2 + j];
+            if (lane < 4) { at[DK] = m[j]; at[DK + 1] = lt[j]; }
+          }
+      }
+      pieces.note(a, cur, item_ends);
+      fresh = true;
+    }
+    if (CLUSTER) ++cur.blk;
+    else step(a, L::KT, cur);
+  }
+  cp_async_wait<0>();
+  if (CLUSTER) {
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float lt = l[j];
+#pragma unroll
+      for (int of = 4; of < 32; of <<= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
+      float* at = reinterpret_cast<float*>(keys.ring) + (quad * 2 + j) * (DK + 2);
+#pragma unroll
+      for (int t = 0; t < NT * 2; ++t) at[t * 8 + (lane >> 2)] = o[t / 2][(t & 1) * 2 + j];
+      if (lane < 4) { at[DK] = m[j]; at[DK + 1] = lt; }
+    }
+    finish_cluster<bf16, DK, RT>(a, cur, smem, L::RING);
+  } else {
+    finish_cta<bf16, DK, RT>(a, pieces.meta);
+  }
+}
+
+template <int DK, bool CLUSTER>
+__global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_rows16_kernel(const __grid_constant__ AttnParams a) {
+  pdl_sync();
+  using L = Mma<DK>;
+  constexpr int RT = 16, NH = 2;         // row halves: this lane's rows are lane / 4 (+ 8)
+  constexpr int KS = DK / 16, NG = L::KT / 16, NT = DK / 8, CN = 4;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, quad = lane & 3;
+  uint32_t* vmask = reinterpret_cast<uint32_t*>(smem + kWarps * L::RING) + w * L::STAGES;
+
+  int64_t x0, x1;
+  Place cur = {};
+  if (CLUSTER) cluster_share(a, L::KT, x0, x1, cur);
+  else find_share(a, L::KT, x0, x1, cur);
+  Pieces pieces;
+  pieces.starts_here = cur.blk == 0;
+  float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * (DK + 2);
+  KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, lane);
+
+  uint32_t qf[KS][4];                    // A operand: columns 16 ks + 2 quad (+ 8), rows lane / 4 (+ 8)
   float m[NH], l[NH], o[NT][CN], far[NH], add[NG * 2][CN] = {}, next[NG * 2][CN] = {};
   const float* bias[NH];
   int len[NH], min_len = 0;      // keys this lane's rows see; the fewest of any row
@@ -833,8 +1108,8 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
           uint32_t b[4];
           const int row = g * 16 + (lane & 7) + ((lane >> 4) & 1) * 8;
           ldsm4(kt + row * L::ROW + swz<L::CPR>(row, 2 * ks + ((lane >> 3) & 1)) * 16, b);
-          mma16816<H16>(s[2 * g], qf[ks][0], qf[ks][NH - 1], qf[ks][NH], qf[ks][2 * NH - 1], b[0], b[1]);
-          mma16816<H16>(s[2 * g + 1], qf[ks][0], qf[ks][NH - 1], qf[ks][NH], qf[ks][2 * NH - 1], b[2], b[3]);
+          mma16816(s[2 * g], qf[ks], b[0], b[1]);
+          mma16816(s[2 * g + 1], qf[ks], b[2], b[3]);
         }
       }
       // scores: scale, bias, mask
@@ -887,35 +1162,23 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
         }
       // Keys that one row sees and another does not have weight 0 there, and 0 x NaN would spoil the row: if such a tile
       // holds a value that is not finite, it is taken key by key.
-      bool plain = false;
-      if (min_len < min(j0 + L::KT, cur.len)) {
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < L::BYTES / 512; ++i) {
-          const uint4 u = *reinterpret_cast<const uint4*>(keys.ring + stage * 2 * L::BYTES + L::BYTES + (i * 32 + lane) * 16);
-          bad |= not_finite(u.x) | not_finite(u.y) | not_finite(u.z) | not_finite(u.w);
-        }
-        plain = __any_sync(0xffffffffu, bad);
-      }
+      const unsigned char* values = keys.ring + stage * 2 * L::BYTES + L::BYTES;
+      const bool plain = min_len < min(j0 + L::KT, cur.len) && tile_not_finite<DK, L::BYTES>(values, lane);
       if (!plain) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          uint32_t hi[4] = {0u, 0u, 0u, 0u}, lo[4] = {0u, 0u, 0u, 0u};
-          split2(s[2 * g][0], s[2 * g][1], hi[0], lo[0]);
-          split2(s[2 * g + 1][0], s[2 * g + 1][1], hi[2], lo[2]);
-          if (H16) {
-            split2(s[2 * g][CN - 2], s[2 * g][CN - 1], hi[1], lo[1]);
-            split2(s[2 * g + 1][CN - 2], s[2 * g + 1][CN - 1], hi[3], lo[3]);
-          }
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) split2(s[2 * g + i / 2][2 * (i & 1)], s[2 * g + i / 2][2 * (i & 1) + 1], hi[i], lo[i]);
 #pragma unroll
           for (int t = 0; t < NT; t += 2) {
             uint32_t b[4];
             const int row = g * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
             ldsm4_t(vt + row * L::ROW + swz<L::CPR>(row, t + ((lane >> 4) & 1)) * 16, b);
-            mma16816<H16>(o[t], hi[0], hi[1], hi[2], hi[3], b[0], b[1]);
-            mma16816<H16>(o[t + 1], hi[0], hi[1], hi[2], hi[3], b[2], b[3]);
-            mma16816<H16>(o[t], lo[0], lo[1], lo[2], lo[3], b[0], b[1]);
-            mma16816<H16>(o[t + 1], lo[0], lo[1], lo[2], lo[3], b[2], b[3]);
+            mma16816(o[t], hi, b[0], b[1]);
+            mma16816(o[t + 1], hi, b[2], b[3]);
+            mma16816(o[t], lo, b[0], b[1]);
+            mma16816(o[t + 1], lo, b[2], b[3]);
           }
         }
       } else {
@@ -925,7 +1188,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_mma_k
         for (int i = 0; i < NG * 2 * CN; ++i) sc[i] = s[i / CN][i % CN];
 #pragma unroll
         for (int i = 0; i < NT * CN; ++i) oc[i] = o[i / CN][i % CN];
-        values_by_key<DK, RT>(keys.ring + stage * 2 * L::BYTES + L::BYTES, sc, oc, len[0] - j0, len[NH - 1] - j0);
+        values_by_key16<DK>(values, sc, oc, len[0] - j0, len[1] - j0);
 #pragma unroll
         for (int i = 0; i < NT * CN; ++i) o[i / CN][i % CN] = oc[i];
       }
@@ -1130,19 +1393,18 @@ cudaError_t run_attention(AttnParams& a, Kernel line, Kernel clustered, int smem
   if (e != cudaSuccess) return e;
   return launch_pdl(paged_attn_join_kernel<T, DK, RT>, dim3(ctas - 1, a.rows), dim3(128), 0, st, a, ctas);
 }
-// Rows of a tile: the float32 kernel's arithmetic goes with them (1, 4, 8), the matrix kernel's softmax by halves (8, 16)
+// Rows of a tile: the float32 kernel's arithmetic goes with them (1, 4, 8), the matrix kernels take 8 or 16
 template <int DK, int RT> cudaError_t run_simt(AttnParams& a, cudaStream_t st) {
   return run_attention<float, DK, RT>(a, paged_attn_simt_kernel<DK, RT, false>, paged_attn_simt_kernel<DK, RT, true>, Simt<DK, RT>::SMEM, st);
-}
-template <int DK, int RT> cudaError_t run_mma(AttnParams& a, cudaStream_t st) {
-  return run_attention<bf16, DK, RT>(a, paged_attn_mma_kernel<DK, RT, false>, paged_attn_mma_kernel<DK, RT, true>, Mma<DK, RT>::SMEM, st);
 }
 template <int DK> cudaError_t run_f32(AttnParams& a, cudaStream_t st) {
   const int rows = a.n_q * a.m;
   return rows == 1 ? run_simt<DK, 1>(a, st) : rows <= 4 ? run_simt<DK, 4>(a, st) : run_simt<DK, 8>(a, st);
 }
 template <int DK> cudaError_t run_bf16(AttnParams& a, cudaStream_t st) {
-  return a.n_q * a.m <= 8 ? run_mma<DK, 8>(a, st) : run_mma<DK, 16>(a, st);
+  if (a.n_q * a.m <= 8)
+    return run_attention<bf16, DK, 8>(a, paged_attn_rows8_kernel<DK, false>, paged_attn_rows8_kernel<DK, true>, Mma<DK>::SMEM, st);
+  return run_attention<bf16, DK, 16>(a, paged_attn_rows16_kernel<DK, false>, paged_attn_rows16_kernel<DK, true>, Mma<DK>::SMEM, st);
 }
 
 }  // namespace

@@ -79,7 +79,11 @@ def check(q, kp, vp, table, lens, scale, n_q, bias):
     ([90, 300], 8, 12, 2, 32, 1, 0, "slots"),
     ([150], 64, 2, 2, 64, 16, 20, "slots"),
     ([70, 333], 1, 40, 2, 64, 16, 0, "heads"),
-    ([50, 61], 3, 64, 2, 128, 128, 500, "slots")])
+    ([50, 61], 3, 64, 2, 128, 128, 500, "slots"),
+    ([400, 0, 33, 1100], 5, 12, 3, 64, 16, 128, "slots"),
+    ([700, 129], 8, 8, 2, 128, 24, 0, "heads"),
+    ([90, 257, 64], 17, 2, 2, 64, 16, 40, "mixed"),
+    ([310, 20], 16, 9, 3, 32, 16, 64, "slots")])
 def test_matches_plain_form(dtype, seq_lens, n_q, h, g, d, page, n_bias, layout, wide):
     rng = np.random.default_rng(len(seq_lens) * 100 + h)
     q, kp, vp, table, lens, bias = build(rng, seq_lens, n_q, h, g, d, page, dtype, layout, n_bias)
@@ -107,7 +111,7 @@ def test_lengths_of_a_sequences_rows_in_no_order(dtype, wide):
     check(q, kp, vp, table, lens, 0.125, 6, bias)
 
 
-@pytest.mark.parametrize("dtype,n_q,h,g", [(F32, 4, 4, 4), (BF16, 4, 4, 4), (BF16, 4, 8, 2), (BF16, 8, 8, 2)])
+@pytest.mark.parametrize("dtype,n_q,h,g", [(F32, 4, 4, 4), (BF16, 4, 4, 4), (BF16, 4, 8, 2), (BF16, 8, 8, 2), (BF16, 11, 4, 2), (BF16, 20, 6, 2)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("wide", [False, True])
 def test_keys_a_row_does_not_see_may_hold_anything(dtype, n_q, h, g, bad, wide):
