@@ -32,8 +32,8 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 // CTAs of a grid at most: 148 SMs, two CTAs each (their rings take 96 KB), four with the smaller rings of narrow heads
 constexpr int max_ctas(int d_kv) { return 148 * (d_kv <= 32 ? 4 : 2); }
-constexpr int kMaxCtas = max_ctas(32);
 constexpr float kLog2e = 1.4426950408889634f;
+template <int DK> constexpr int kRowOf = DK + 4;      // floats of a piece's row: output, maximum, sum, two unused (16-byte rows)
 
 struct AttnParams {
   const char* q;
@@ -50,8 +50,8 @@ struct AttnParams {
   int cap;               // keys a page table row can name
   PagedPool pool;
   int runs;              // 1: pages hold whole runs of keys (KeyStream)
-  float* warp_part;      // [workers][2][rows][d + 2]: output, maximum, sum of the pieces a warp leaves
-  float* part;           // [ctas][2][rows][d + 2]: the same of a CTA
+  float* warp_part;      // [workers][2][rows][d + 4]: output, maximum, sum of the pieces a warp leaves
+  float* part;           // [ctas][2][rows][d + 4]: the same of a CTA
   int4* meta;            // [ctas]: which pieces those are, see below
   int cluster;           // CTAs per item when every item has a cluster of its own
   int extra;             // tiles that an item counts beside its own (find_share)
@@ -350,7 +350,7 @@ __device__ void finish_cta(const AttnParams& a, const int4& mine) {
   if (lane == 0) metas[tid >> 5] = mine;
   __syncthreads();      // also orders the warps' pieces in global memory before the reads below
   constexpr int VC = DK / 32;
-  const int64_t piece = (int64_t)a.rows * (DK + 2);
+  const int64_t piece = (int64_t)a.rows * kRowOf<DK>;
   const float* parts = a.warp_part + (int64_t)blockIdx.x * kWarps * 2 * piece;
   int4 meta = make_int4(metas[0].x, 0, -1, 0);
   int turn = 0;      // rows seen so far: warp w takes those with turn % kWarps == w
@@ -373,7 +373,7 @@ __device__ void finish_cta(const AttnParams& a, const int4& mine) {
       float mx = -INFINITY, sum = 0.f, pm[kWarps], pl[kWarps], v[kWarps][VC], acc[VC];
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) {
-        const float* q = first + (i == 0 ? 0 : second + (i - 1) * 2 * piece) + r * (DK + 2);
+        const float* q = first + (i == 0 ? 0 : second + (i - 1) * 2 * piece) + r * kRowOf<DK>;
         pm[i] = -INFINITY; pl[i] = 0.f;
         if (i < n) { pm[i] = q[DK]; pl[i] = q[DK + 1]; }
 #pragma unroll
@@ -397,7 +397,7 @@ __device__ void finish_cta(const AttnParams& a, const int4& mine) {
         for (int c = 0; c < VC; ++c) out_row<T, DK>(a, row, h)[lane + 32 * c] = from_f<T>(sum == 0.f ? 0.f : acc[c] / sum);
         if (lane == 0) write_lse(a, row, h, mx, sum);
       } else {
-        float* pt = a.part + ((int64_t)blockIdx.x * 2 + (w < 0 ? 0 : 1)) * piece + r * (DK + 2);
+        float* pt = a.part + ((int64_t)blockIdx.x * 2 + (w < 0 ? 0 : 1)) * piece + r * kRowOf<DK>;
 #pragma unroll
         for (int c = 0; c < VC; ++c) pt[lane + 32 * c] = acc[c];
         if (lane == 0) { pt[DK] = mx; pt[DK + 1] = sum; }
@@ -422,7 +422,7 @@ __device__ __forceinline__ void cluster_share(const AttnParams& a, int bk, int64
   if (blockIdx.x == item * a.cluster && p.k == 0 && threadIdx.x < a.n_q && a.lens[p.s * a.n_q + threadIdx.x] > a.cap)
     paged_report(a.status, PAGED_BAD_LENGTH);
 }
-// Joins the warps of a cluster: warp w of each CTA has left its rows ([row][DK + 2]: output, maximum, sum) at smem + w *
+// Joins the warps of a cluster: warp w of each CTA has left its rows ([row][DK + 4]: output, maximum, sum) at smem + w *
 // stride.  A warp of the cluster takes 32 columns of a row; lane i looks at piece i's maximum and sum.
 template <typename T, int DK, int RT>
 __device__ void finish_cluster(const AttnParams& a, const Place& p, unsigned char* smem, int stride) {
@@ -434,7 +434,7 @@ __device__ void finish_cluster(const AttnParams& a, const Place& p, unsigned cha
   for (int unit = rank * kWarps + (threadIdx.x >> 5); unit < rows.n * (DK / 32); unit += n) {
     const int r = unit / (DK / 32), c = unit % (DK / 32) * 32 + lane;
     auto piece = [&](int i) {
-      return reinterpret_cast<const float*>(cluster.map_shared_rank(smem + (i % kWarps) * stride, i / kWarps)) + r * (DK + 2);
+      return reinterpret_cast<const float*>(cluster.map_shared_rank(smem + (i % kWarps) * stride, i / kWarps)) + r * kRowOf<DK>;
     };
     float m = -INFINITY, l = 0.f;
     if (lane < n) { m = piece(lane)[DK]; l = piece(lane)[DK + 1]; }
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
   else find_share(a, L::KT, x0, x1, cur);
   Pieces pieces;
   pieces.starts_here = cur.blk == 0;
-  float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * (DK + 2);
+  float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * kRowOf<DK>;
   KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, lane);
 
   const int key_l = lane % L::KT, part_l = lane / L::KT;
@@ -632,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
           for (int of = 16; of > 0; of >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
           const bool whole = pieces.whole(item_ends);
           const int h = head[r], row = q_row[r];
-          float* at = whole ? out_row<float, DK>(a, row, h) : part + (pieces.slot() * a.rows + r) * (DK + 2);
+          float* at = whole ? out_row<float, DK>(a, row, h) : part + (pieces.slot() * a.rows + r) * kRowOf<DK>;
 #pragma unroll
           for (int c = 0; c < L::VC; ++c) at[lane * L::VC + c] = !whole ? o[r][c] : (lt == 0.f ? 0.f : o[r][c] / lt);
           if (lane == 0) {
@@ -655,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
       float lt = part_l == 0 ? l[r] : 0.f;
 #pragma unroll
       for (int of = 16; of > 0; of >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
-      float* at = reinterpret_cast<float*>(keys.ring) + r * (DK + 2);
+      float* at = reinterpret_cast<float*>(keys.ring) + r * kRowOf<DK>;
 #pragma unroll
       for (int c = 0; c < L::VC; ++c) at[lane * L::VC + c] = o[r][c];
       if (lane == 0) { at[DK] = m[r]; at[DK + 1] = lt; }
@@ -772,7 +772,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_rows8
   else find_share(a, L::KT, x0, x1, cur);
   Pieces pieces;
   pieces.starts_here = cur.blk == 0;
-  float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * (DK + 2);
+  float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * kRowOf<DK>;
   KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, lane);
 
   uint32_t qf[KS][2];                    // B operand: columns 16 ks + 2 quad (+ 8) of row lane / 4
@@ -974,7 +974,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_rows8
 #pragma unroll
         for (int j = 0; j < 2; ++j)
           if (quad * 2 + j < rows.n) {
-            float* at = part + (pieces.slot() * a.rows + quad * 2 + j) * (DK + 2);
+            float* at = part + (pieces.slot() * a.rows + quad * 2 + j) * kRowOf<DK>;
 #pragma unroll
             for (int t = 0; t < NT * 2; ++t) at[t * 8 + (lane >> 2)] = o[t / 2][(t & 1) * 2 + j];
             if (lane < 4) { at[DK] = m[j]; at[DK + 1] = lt[j]; }
@@ -994,7 +994,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_rows8
       float lt = l[j];
 #pragma unroll
       for (int of = 4; of < 32; of <<= 1) lt += __shfl_xor_sync(0xffffffffu, lt, of);
-      float* at = reinterpret_cast<float*>(keys.ring) + (quad * 2 + j) * (DK + 2);
+      float* at = reinterpret_cast<float*>(keys.ring) + (quad * 2 + j) * kRowOf<DK>;
 #pragma unroll
       for (int t = 0; t < NT * 2; ++t) at[t * 8 + (lane >> 2)] = o[t / 2][(t & 1) * 2 + j];
       if (lane < 4) { at[DK] = m[j]; at[DK + 1] = lt; }
@@ -1021,7 +1021,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_rows1
   else find_share(a, L::KT, x0, x1, cur);
   Pieces pieces;
   pieces.starts_here = cur.blk == 0;
-  float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * (DK + 2);
+  float* part = a.warp_part + ((int64_t)blockIdx.x * kWarps + w) * 2 * a.rows * kRowOf<DK>;
   KeyStream<L> keys(a, cur, x1 - x0, smem + w * L::RING, vmask, lane);
 
   uint32_t qf[KS][4];                    // A operand: columns 16 ks + 2 quad (+ 8), rows lane / 4 (+ 8)
@@ -1221,7 +1221,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_rows1
               *reinterpret_cast<__nv_bfloat162*>(at + t * 8) = __floats2bfloat162_rn(o[t][2 * hf] * inv, o[t][2 * hf + 1] * inv);
             if (quad == 0) write_lse(a, row, h, m[hf], lt);
           } else {
-            float* at = part + (pieces.slot() * a.rows + r) * (DK + 2);
+            float* at = part + (pieces.slot() * a.rows + r) * kRowOf<DK>;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
               *reinterpret_cast<float2*>(at + t * 8 + quad * 2) = make_float2(o[t][2 * hf], o[t][2 * hf + 1]);
@@ -1243,7 +1243,7 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_rows1
       float lt = l[hf];
       lt += __shfl_xor_sync(0xffffffffu, lt, 1);
       lt += __shfl_xor_sync(0xffffffffu, lt, 2);
-      float* at = reinterpret_cast<float*>(keys.ring) + (lane / 4 + 8 * hf) * (DK + 2);
+      float* at = reinterpret_cast<float*>(keys.ring) + (lane / 4 + 8 * hf) * kRowOf<DK>;
 #pragma unroll
       for (int t = 0; t < NT; ++t)
         *reinterpret_cast<float2*>(at + t * 8 + quad * 2) = make_float2(o[t][2 * hf], o[t][2 * hf + 1]);
@@ -1256,73 +1256,87 @@ __global__ void __launch_bounds__(kThreads, max_ctas(DK) / 148) paged_attn_rows1
 }
 
 // Joins the pieces of the item that the boundary behind CTA blockIdx.x is the first to cut; one CTA per boundary and query
-// row.
+// row.  Its warps take every kJoinWarps-th piece, eight at a time with all their loads on the way at once, and combine what
+// they have in shared memory (74 pieces of an item, one sequence of 46,900 keys: 11 us with separate passes for maxima, sums
+// and columns, 7 us so).
+constexpr int kJoinWarps = 4;
 template <typename T, int DK, int RT>
-__global__ void __launch_bounds__(128) paged_attn_join_kernel(const __grid_constant__ AttnParams a, int ctas) {
+__global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const __grid_constant__ AttnParams a, int ctas) {
   pdl_sync();
   const int c0 = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int item = a.meta[c0].z;
+  // pieces: slot 1 of c0, then slot 0 of the CTAs behind it up to the one where the item ends (a CTA without work lies
+  // between items, never inside one)
+  int4 mt = a.meta[min(c0 + 1 + lane, ctas - 1)];
   if (item < 0) return;
+  int last = ctas - 1;
+  for (int c = c0 + 1; c < ctas; c += 32) {      // every warp looks for itself
+    if (c > c0 + 1) mt = a.meta[min(c + lane, ctas - 1)];
+    const uint32_t ends = __ballot_sync(0xffffffffu, c + lane < ctas && !(mt.x == item && mt.y == 1));
+    if (ends) { last = c + __ffs(ends) - 1; break; }
+  }
   const Place p = item_place(a, item);
   const Rows rows(a, p, RT);
   if (r >= rows.n) return;
-  // pieces: slot 1 of c0, then slot 0 of the CTAs behind it up to the one where the item ends (a CTA without work lies
-  // between items, never inside one)
-  __shared__ int s_last;
-  if (tid == 0) s_last = ctas - 1;
-  __syncthreads();
-  for (int c = c0 + 1 + tid; c < ctas; c += 128) {
-    const int4 mt = a.meta[c];
-    if (!(mt.x == item && mt.y == 1)) { atomicMin(&s_last, c); break; }
-  }
-  __syncthreads();
-  const int n = s_last - c0 + 1;
-  auto piece = [&](int i) {
-    return a.part + (((int64_t)(c0 + i) * 2 + (i == 0 ? 1 : 0)) * a.rows + r) * (DK + 2);
-  };
-  // the weights of all pieces first, then their columns: every load of a pass is independent of the others
-  __shared__ float weight[kMaxCtas], top[4], sums[4];
-  float mx = -INFINITY;
-  for (int i = tid; i < n; i += 128) {
-    weight[i] = piece(i)[DK];
-    mx = fmaxf(mx, weight[i]);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-  if (lane == 0) top[w] = mx;
-  __syncthreads();
-  mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-  const float ref = mx == -INFINITY ? 0.f : mx;
-  float sum = 0.f;
-  for (int i = tid; i < n; i += 128) {
-    weight[i] = ex2((weight[i] - ref) * kLog2e);
-    sum += weight[i] * piece(i)[DK + 1];
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (lane == 0) sums[w] = sum;
-  __syncthreads();
-  sum = sums[0] + sums[1] + sums[2] + sums[3];
-  // four warps take every fourth piece; a lane holds DK / 32 columns
+  const int n = last - c0 + 1;
   constexpr int VC = DK / 32;
-  __shared__ float red[4][DK];
-  float acc[VC];
+  struct alignas(VC * 4) Cols { float v[VC]; };
+  float mx = -INFINITY, sum = 0.f, acc[VC];
 #pragma unroll
   for (int c = 0; c < VC; ++c) acc[c] = 0.f;
-#pragma unroll 8
-  for (int i = w; i < n; i += 4) {
-    const float* pt = piece(i);
+  for (int i0 = w; i0 < n; i0 += 8 * kJoinWarps) {
+    float2 ms[8];      // maximum and sum
+    Cols v[8];
+    float top = mx;
 #pragma unroll
-    for (int c = 0; c < VC; ++c) acc[c] += weight[i] * pt[lane + 32 * c];
+    for (int k = 0; k < 8; ++k) {
+      const int i = i0 + k * kJoinWarps;
+      ms[k] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int c = 0; c < VC; ++c) v[k].v[c] = 0.f;
+      if (i < n) {
+        const float* q = a.part + (((int64_t)(c0 + i) * 2 + (i == 0 ? 1 : 0)) * a.rows + r) * kRowOf<DK>;
+        ms[k] = *reinterpret_cast<const float2*>(q + DK);
+        v[k] = *reinterpret_cast<const Cols*>(q + lane * VC);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = fmaxf(top, ms[k].x);
+    const float ref = top == -INFINITY ? 0.f : top;
+    const float f = ex2((mx - ref) * kLog2e);
+    mx = top;
+    sum *= f;
+#pragma unroll
+    for (int c = 0; c < VC; ++c) acc[c] *= f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float e = ex2((ms[k].x - ref) * kLog2e);
+      sum += e * ms[k].y;
+#pragma unroll
+      for (int c = 0; c < VC; ++c) acc[c] += e * v[k].v[c];
+    }
   }
+  __shared__ float red[kJoinWarps][DK], red_m[kJoinWarps], red_s[kJoinWarps];
 #pragma unroll
-  for (int c = 0; c < VC; ++c) red[w][lane + 32 * c] = acc[c];
+  for (int c = 0; c < VC; ++c) red[w][lane * VC + c] = acc[c];
+  if (lane == 0) { red_m[w] = mx; red_s[w] = sum; }
   __syncthreads();
   if (tid < DK) {
-    const float v = red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid];
+    mx = red_m[0];
+#pragma unroll
+    for (int i = 1; i < kJoinWarps; ++i) mx = fmaxf(mx, red_m[i]);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float out = 0.f;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinWarps; ++i) {
+      const float e = ex2((red_m[i] - ref) * kLog2e);
+      out += e * red[i][tid];
+      sum += e * red_s[i];
+    }
     int row, h;
     rows.place(a, p, r, row, h);
-    out_row<T, DK>(a, row, h)[tid] = from_f<T>(sum == 0.f ? 0.f : v / sum);
+    out_row<T, DK>(a, row, h)[tid] = from_f<T>(sum == 0.f ? 0.f : out / sum);
     if (tid == 0) write_lse(a, row, h, mx, sum);
   }
 }
@@ -1391,7 +1405,7 @@ cudaError_t run_attention(AttnParams& a, Kernel line, Kernel clustered, int smem
   a.extra = a.bias != nullptr ? 2 : 1;
   e = launch_pdl(line, dim3(ctas), dim3(kThreads), (size_t)smem, st, a);
   if (e != cudaSuccess) return e;
-  return launch_pdl(paged_attn_join_kernel<T, DK, RT>, dim3(ctas - 1, a.rows), dim3(128), 0, st, a, ctas);
+  return launch_pdl(paged_attn_join_kernel<T, DK, RT>, dim3(ctas - 1, a.rows), dim3(kJoinWarps * 32), 0, st, a, ctas);
 }
 // Rows of a tile: the float32 kernel's arithmetic goes with them (1, 4, 8), the matrix kernels take 8 or 16
 template <int DK, int RT> cudaError_t run_simt(AttnParams& a, cudaStream_t st) {
@@ -1413,7 +1427,7 @@ int64_t paged_attention_workspace(int n_rows, int n_q, int H, int Hkv, int d_kv)
   (void)n_rows;
   const int64_t all = (int64_t)n_q * (H / Hkv), rows = all < 16 ? all : 16;
   const int64_t ctas = max_ctas(d_kv);
-  return ctas * (int64_t)sizeof(int4) + ctas * (1 + kWarps) * 2 * rows * (d_kv + 2) * 4;
+  return ctas * (int64_t)sizeof(int4) + ctas * (1 + kWarps) * 2 * rows * (d_kv + 4) * 4;
 }
 
 cudaError_t launch_paged_attention(const PagedAttnArgs& g, cudaStream_t st) {
@@ -1429,7 +1443,7 @@ cudaError_t launch_paged_attention(const PagedAttnArgs& g, cudaStream_t st) {
   a.meta = (int4*)g.workspace;
   const int rows = a.n_q * a.m < 16 ? a.n_q * a.m : 16;
   a.part = (float*)((char*)g.workspace + max_ctas(g.d_kv) * sizeof(int4));
-  a.warp_part = a.part + (int64_t)max_ctas(g.d_kv) * 2 * rows * (g.d_kv + 2);
+  a.warp_part = a.part + (int64_t)max_ctas(g.d_kv) * 2 * rows * (g.d_kv + 4);
   if (g.dtype == DT_F32) return g.d_kv == 32 ? run_f32<32>(a, st) : g.d_kv == 64 ? run_f32<64>(a, st) : run_f32<128>(a, st);
   return g.d_kv == 32 ? run_bf16<32>(a, st) : g.d_kv == 64 ? run_bf16<64>(a, st) : run_bf16<128>(a, st);
 }
