@@ -555,6 +555,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
           sc[r] = fmaf(q4.z, k4.z, sc[r]); sc[r] = fmaf(q4.w, k4.w, sc[r]);
         }
       }
+      // a tile's keys are summed by themselves and then added: KT + n / KT roundings instead of n
+      float corr[RT], t[RT][L::VC];
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int c = 0; c < L::VC; ++c) t[r][c] = 0.f;
       bool all_see = true;      // every row sees every key of the tile that exists
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
@@ -568,12 +574,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
         for (int of = 16; of > 0; of >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, of));
         mx = fmaxf(m[r], mx);
         const float ref = mx == -INFINITY ? 0.f : mx;
-        const float corr = ex2((m[r] - ref) * kLog2e);
+        corr[r] = ex2((m[r] - ref) * kLog2e);
         sc[r] = ex2((s - ref) * kLog2e);
         m[r] = mx;
-        l[r] = l[r] * corr + sc[r];
-#pragma unroll
-        for (int c = 0; c < L::VC; ++c) o[r][c] *= corr;
+        l[r] = l[r] * corr[r] + sc[r];
       }
       if (RT > 1) {      // the weights in shared memory: two loads give a key's weights of eight rows
         __syncwarp();
@@ -594,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
           const Cols vf = values(kk);
           const float p = __shfl_sync(0xffffffffu, sc[0], kk);
 #pragma unroll
-          for (int c = 0; c < L::VC; ++c) o[0][c] = fmaf(p, vf.v[c], o[0][c]);
+          for (int c = 0; c < L::VC; ++c) t[0][c] = fmaf(p, vf.v[c], t[0][c]);
         }
       } else if (all_see) {
 #pragma unroll 8
@@ -604,7 +608,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
           for (int r = 0; r < RT; ++r) {
             const float p = ps[kk * RT + r];
 #pragma unroll
-            for (int c = 0; c < L::VC; ++c) o[r][c] = fmaf(p, vf.v[c], o[r][c]);
+            for (int c = 0; c < L::VC; ++c) t[r][c] = fmaf(p, vf.v[c], t[r][c]);
           }
         }
       } else {
@@ -616,10 +620,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_attn_simt_kernel(const __gr
           for (int r = 0; r < RT; ++r) {
             const float p = ps[kk * RT + r];
 #pragma unroll
-            for (int c = 0; c < L::VC; ++c) o[r][c] = j0 + kk < len[r] ? fmaf(p, vf.v[c], o[r][c]) : o[r][c];
+            for (int c = 0; c < L::VC; ++c) t[r][c] = j0 + kk < len[r] ? fmaf(p, vf.v[c], t[r][c]) : t[r][c];
           }
         }
       }
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int c = 0; c < L::VC; ++c) o[r][c] = fmaf(o[r][c], corr[r], t[r][c]);
     }
     stage = (stage + 1) % L::STAGES;
     const bool item_ends = cur.blk + 1 == cur.nb;
