@@ -443,10 +443,11 @@ T5_API int t5_paged_attention(int32_t dtype, int32_t n_rows, int32_t n_q, int32_
 /* Verification of drafted tokens from given random numbers.  Sequence s has n = d_n_draft[s] (NULL: max_draft) tokens
  * x_i = d_draft_tokens[s * ld_draft_tokens + i]; target_i = row i of the target's probabilities (rows 0 .. n: at
  * d_target + s * target_seq_stride + i * target_row_stride, vocab values), draft_i likewise (d_draft NULL: draft_i is one
- * at x_i, the token was not drawn).  x_0, x_1, ... are accepted while u_i draft_i(x_i) < target_i(x_i) with
- * u_i = d_u_accept[s * ld_u_accept + i] in [0, 1).  Behind the a accepted ones token y is drawn from
- * r = max(target_a - draft_a, 0) if x_a was refused, from r = target_n if none was:  the first y with
- * sum_{v <= y} r_v > d_u_sample[s] sum_v r_v, in float64.  Values that are not positive and finite count as 0; if that
+ * at x_i, the token was not drawn).  The arrays hold max_draft tokens and rows of every sequence, whatever n is.
+ * x_0, x_1, ... are accepted while u_i draft_i(x_i) < target_i(x_i) with u_i = d_u_accept[s * ld_u_accept + i] in [0, 1).
+ * Behind the a accepted ones token y is drawn from r = max(target_a - draft_a, 0) if x_a was refused, from r = target_n if
+ * none was:  the first y with sum_{v <= y} r_v > d_u_sample[s] sum_v r_v, in float64, d_u_sample in [0, 1) (a value below
+ * and NaN: the first y with r_y > 0; a value above: the last).  Values that are not positive and finite count as 0; if that
  * leaves nothing of a difference the token is drawn from target_a, and if that has nothing either it is -1.  A drafted
  * token outside [0, vocab) is refused.
  * Writes d_out_tokens[s * ld_out_tokens + 0 .. max_draft] = accepted tokens, y, then -1, and d_n_accepted[s] = a.

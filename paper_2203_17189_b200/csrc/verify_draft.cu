@@ -21,6 +21,7 @@
 #include <cooperative_groups.h>
 #include <math.h>
 #include <string.h>
+#include <utility>
 
 namespace cg = cooperative_groups;
 
@@ -136,7 +137,8 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
   __shared__ int first, run_at;
   const int K = a.K, V = a.V;
   const int n = a.n_draft != nullptr ? min(max(a.n_draft[s], 0), K) : K;
-  const double u = a.u_sample[s];
+  const double u = fmax((double)a.u_sample[s], 0.0);      // below 0 and NaN: 0, so that what it draws has mass
+  auto started = cluster.barrier_arrive();      // waited for where the CTAs first write to each other
   if (tid == 0) { first = K; run_at = -1; }
   __syncthreads();
   const T* tgt = reinterpret_cast<const T*>(a.target) + s * a.t_seq;
@@ -169,6 +171,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
     const int skip = attempt == 0 ? hole : -1;
     if (d != nullptr) sum_runs<T, LN, true>(tr, d, r0, r1 - r0, V, a.vec, skip, runs);
     else sum_runs<T, LN, false>(tr, d, r0, r1 - r0, V, a.vec, skip, runs);
+    if (attempt == 0) cluster.barrier_wait(std::move(started));
     __syncthreads();
     // inclusive prefix sums of the runs
     if (w == 0) {

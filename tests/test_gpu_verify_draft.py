@@ -125,6 +125,27 @@ def test_random_numbers_at_the_ends():
     check(target, draft, tokens, None, ua, np.array([0.0, 1.0, np.nextafter(np.float32(1), np.float32(0)), 0.0], np.float32))
 
 
+@pytest.mark.parametrize("s,v", [(3, 5), (3, 700), (3, 32128), (200, 90)])
+def test_random_numbers_out_of_range(s, v):
+    """Below the range, and NaN: the first token with mass; above it: the last."""
+    target = torch.zeros(s, 1, v, device=DEV)
+    target[:, 0, 2:v - 1] = 0.25
+    us = np.resize(np.array([-0.5, np.nan, 7.0, -np.inf, np.inf, -1e-30], np.float32), s)
+    out, acc = run(target, None, np.zeros((s, 0), np.int32), None, np.zeros((s, 0), np.float32), us)
+    np.testing.assert_array_equal(out[:, 0], np.where(us > 1, v - 2, 2))
+    assert (acc == 0).all()
+
+
+def test_output_over_the_drafted_tokens():
+    rng = np.random.default_rng(10)
+    target, draft, tokens, ua, us = inputs(rng, 7, 3, 900, torch.float32, True)
+    want, _ = run(target, draft, tokens, None, ua, us)
+    over, acc = torch.zeros(7, 4, dtype=torch.int32, device=DEV), torch.empty(7, dtype=torch.int32, device=DEV)
+    over[:, :3] = dev(tokens, torch.int32)
+    Bd.t5_verify_draft(target, draft, over[:, :3], None, dev(ua, torch.float32), dev(us, torch.float32), over, acc)
+    np.testing.assert_array_equal(over.cpu().numpy(), want)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_strides(dtype):
     """Rows on no 16-byte boundary, and positions outermost."""
