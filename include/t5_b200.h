@@ -205,8 +205,8 @@ T5_API int t5_decode_step(t5_handle* h, const void* d_params, void* d_cache, int
  *    of values, [n_pages, page_size, heads, d_kv] each.  One page table serves all layers.
  *  - d_tokens, d_positions [S * n_new]: decoder INPUT tokens (0 at position 0) and their positions; a negative position
  *    is an unused slot (its token must be a valid id, its logits are undefined).  A token sees its sequence's positions
- *    up to its own, those of this call included; a position may be written again (a refused draft), what lies behind the
- *    last written position is never read.
+ *    up to its own, those of this call included; a later call may write a position again (a refused draft), two tokens of
+ *    one call may not share one.  What lies behind a token's own position is never read.
  *  - encoder-decoder: d_cross_cache is a cache filled by t5_decode_begin(B = S, Te, Tmax = 1); else NULL with Te = 0.
  *  - d_logits [S * n_new, vocab] in the configured dtype.
  * A token that finds no page leaves a code for t5_device_status(d_workspace). */

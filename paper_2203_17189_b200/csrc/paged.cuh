@@ -36,6 +36,12 @@ struct PagedPool {
   FastDiv ps;
 };
 
+// Code of a launch; the runtime's record of a failed one is cleared, so that the next call does not report it again
+inline int paged_result(cudaError_t e) {
+  if (e == cudaSuccess) return 0;
+  cudaGetLastError();
+  return -6;      // T5_ERR_CUDA
+}
 inline bool paged_aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // Checks shared by the calls that take pools; fills `out`.  Returns a T5_ERR_* code.

@@ -256,6 +256,7 @@ extern "C" int t5_paged_kv_append(int32_t dtype, int32_t n_tokens, int32_t n_hea
                                   int64_t slot_stride, int64_t head_stride, const int32_t* d_page_table, int32_t n_seqs,
                                   int32_t max_pages, int64_t ld_table, void* stream) {
   if (dtype != DT_F32 && dtype != DT_BF16) return T5_ERR_ARG;
+  if (n_tokens == 0) return T5_OK;
   const int es = dtype == DT_F32 ? 4 : 2;
   PagedAppendArgs a;
   memset(&a, 0, sizeof a);
@@ -266,7 +267,6 @@ extern "C" int t5_paged_kv_append(int32_t dtype, int32_t n_tokens, int32_t n_hea
   if (rot_dim < 0 || rot_dim > d_kv || rot_dim % 16 || (rot_interleaved != 0 && rot_interleaved != 1)) return T5_ERR_ARG;
   if (rot_dim > 0 && !(rot_base > 0.0 && rot_base < 1e300)) return T5_ERR_ARG;
   if ((d_q == nullptr) != (d_q_out == nullptr)) return T5_ERR_NULL;
-  if (n_tokens == 0) return T5_OK;
   if (!d_k || !d_v || !d_seq || !d_positions) return T5_ERR_NULL;
   if (d_q != nullptr && (n_heads < 1 || n_heads > 4096 || ldq < (int64_t)n_heads * d_kv || ldqo < (int64_t)n_heads * d_kv))
     return T5_ERR_ARG;
@@ -278,5 +278,5 @@ extern "C" int t5_paged_kv_append(int32_t dtype, int32_t n_tokens, int32_t n_hea
   a.q = d_q; a.k = d_k; a.v = d_v; a.q_out = d_q_out; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldqo = ldqo;
   a.seq = d_seq; a.pos = d_positions; a.tokens_per_seq = 1; a.rot_dim = rot_dim; a.rot_base = rot_base;
   a.interleaved = rot_interleaved; a.n_seqs = n_seqs; a.status = g_kernel_status;
-  return launch_paged_append(a, (cudaStream_t)stream) == cudaSuccess ? T5_OK : T5_ERR_CUDA;
+  return paged_result(launch_paged_append(a, (cudaStream_t)stream));
 }

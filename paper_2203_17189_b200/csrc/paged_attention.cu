@@ -1351,7 +1351,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
 
 using Kernel = void (*)(AttnParams);
 
-// CTAs that fill the GPU with this kernel, looked up once per device
 // CTAs that fill the GPU with this kernel, looked up (and its shared memory allowed) once per device
 template <typename T, int DK, int RT, bool CLUSTER>
 cudaError_t grid_of(Kernel kernel, int smem, int* ctas) {
@@ -1486,13 +1485,13 @@ int t5_paged_attention(int32_t dtype, int32_t n_rows, int32_t n_q, int32_t n_hea
   const int es = dtype == DT_F32 ? 4 : 2;
   int rc = attention_shape(n_rows, n_q, n_heads, n_kv_heads, d_kv);
   if (rc != T5_OK) return rc;
+  if (n_rows == 0) return T5_OK;
   PagedAttnArgs a;
   memset(&a, 0, sizeof a);
   rc = paged_pool_args(es, n_kv_heads, d_kv, d_k_pages, d_v_pages, n_pages, page_size, page_stride, slot_stride, head_stride,
-                       d_page_table, n_rows > 0 ? n_rows / n_q : 1, max_pages, ld_table, &a.pool);
+                       d_page_table, n_rows / n_q, max_pages, ld_table, &a.pool);
   if (rc != T5_OK) return rc;
   if ((d_bias != nullptr) != (n_bias > 0) || n_bias < 0 || !isfinite(scale)) return T5_ERR_ARG;
-  if (n_rows == 0) return T5_OK;
   if (!d_q || !d_lens || !d_out || !d_workspace) return T5_ERR_NULL;
   if (ldq < (int64_t)n_heads * d_kv || ldo < (int64_t)n_heads * d_kv) return T5_ERR_ARG;
   if (!paged_aligned(d_q) || !paged_aligned(d_out) || !paged_aligned(d_workspace) || (ldq * es) % 16 || (ldo * es) % 16)
@@ -1501,7 +1500,7 @@ int t5_paged_attention(int32_t dtype, int32_t n_rows, int32_t n_q, int32_t n_hea
   a.dtype = dtype; a.n_rows = n_rows; a.n_q = n_q; a.H = n_heads; a.Hkv = n_kv_heads; a.d_kv = d_kv;
   a.q = d_q; a.out = d_out; a.ldq = ldq; a.ldo = ldo; a.lse = d_lse; a.lens = d_lens; a.bias = d_bias; a.n_bias = n_bias;
   a.scale = scale; a.workspace = d_workspace; a.status = g_kernel_status;
-  return launch_paged_attention(a, (cudaStream_t)stream) == cudaSuccess ? T5_OK : T5_ERR_CUDA;
+  return paged_result(launch_paged_attention(a, (cudaStream_t)stream));
 }
 
 }  // extern "C"

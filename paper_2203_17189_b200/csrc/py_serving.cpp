@@ -87,7 +87,7 @@ struct Pools {
     seqs = tb.size(0); max_pages = tb.size(1);
     ld = seqs > 1 ? tb.stride(0) : max_pages;
     k = kp.data_ptr(); v = vp.data_ptr(); table = tb.data_ptr();
-    if (n > INT32_MAX || ps > INT32_MAX || max_pages > INT32_MAX) refuse("pools: sizes beyond 2^31");
+    if (n > INT32_MAX || ps > INT32_MAX || g > INT32_MAX || d > INT32_MAX || seqs > INT32_MAX || max_pages > INT32_MAX) refuse("pools: sizes beyond 2^31");
   }
 };
 int64_t integer(PyObject* o, const char* name) {

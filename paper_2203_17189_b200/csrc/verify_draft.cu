@@ -16,7 +16,7 @@
 // takes one sequence; every warp sums runs of the row, the CTAs exchange their totals through distributed shared memory,
 // and the one warp whose run holds the drawn point reads that run again and finds the token.
 #include "../../include/t5_b200.h"
-#include "common.cuh"
+#include "paged.cuh"
 
 #include <cooperative_groups.h>
 #include <math.h>
@@ -326,5 +326,5 @@ extern "C" int t5_verify_draft(int32_t dtype, int32_t n_seqs, int32_t max_draft,
   const int cs = cluster_size<LN>(n_seqs, vocab);
   const cudaError_t e = dtype == DT_F32 ? run<float, LN>(a, n_seqs, cs, (cudaStream_t)stream)
                                         : run<bf16, LN>(a, n_seqs, cs, (cudaStream_t)stream);
-  return e == cudaSuccess ? T5_OK : T5_ERR_CUDA;
+  return paged_result(e);
 }

@@ -133,6 +133,16 @@ def test_tokens_without_a_place_are_left_out_and_reported():
     assert int((~torch.isnan(kp)).sum()) == 32 and int((~torch.isnan(vp)).sum()) == 32
 
 
+def test_no_tokens_and_all_padding():
+    rng = np.random.default_rng(10)
+    kp, vp, table = SR.make_pools(rng, [32], 16, 2, 32, torch.float32, DEV)
+    q, k, v = make_tokens(rng, 3, 2, 2, 32, torch.float32)
+    Bd.t5_paged_kv_append(k[:0], v[:0], kp, vp, table, i32([]), i32([]), q=q[:0], q_out=q[:0].clone(), rot_dim=32)
+    q_out = torch.empty_like(q)
+    Bd.t5_paged_kv_append(k, v, kp, vp, table, i32([0, 7, -1]), i32([-1, -5, -2 ** 31]), q=q, q_out=q_out, rot_dim=32)
+    assert torch.isnan(kp).all() and torch.isnan(vp).all() and torch.equal(q_out, q)
+
+
 def test_binding_refuses_wrong_tensors():
     rng = np.random.default_rng(9)
     kp, vp, table = SR.make_pools(rng, [32], 16, 2, 32, torch.float32, DEV)

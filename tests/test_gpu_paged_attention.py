@@ -293,6 +293,18 @@ def test_two_streams_with_a_workspace_each():
     assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
 
 
+def test_empty_batch_and_output_over_the_queries():
+    rng = np.random.default_rng(22)
+    q, kp, vp, table, lens, _ = build(rng, [300, 41], 1, 4, 2, 64, 16, BF16)
+    ws = workspace(2, 1, 4, 2, 64)
+    Bd.t5_paged_attention(q[:0], kp, vp, table[:0], i32([]), q[:0], ws)
+    for wide in (table, widened(table, 16)):
+        want, _ = attend(q, kp, vp, wide, lens, 0.1, 1, None, ws)
+        over = q.clone()
+        Bd.t5_paged_attention(over, kp, vp, wide, i32(lens), over, ws, scale=0.1)
+        assert torch.equal(over, want)
+
+
 def test_binding_refuses_wrong_tensors():
     rng = np.random.default_rng(21)
     q, kp, vp, table, lens, bias = build(rng, [30, 30], 1, 4, 2, 64, 16, BF16, n_bias=8)
