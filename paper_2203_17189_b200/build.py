@@ -13,7 +13,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libt5b200.so")
 PY_LIB = os.path.join(HERE, "_serving.so")      # Python side of the serving calls (csrc/py_serving.cpp)
 SOURCES = ["t5_model.cu", "elementwise.cu", "gemm_simt.cu", "gemm_tcgen05.cu", "attention_simt.cu", "attention_tc.cu",
-           "relbias.cu", "noalloc.cu", "selftest.cu", "paged_append.cu", "paged_attention.cu", "verify_draft.cu"]
+           "relbias.cu", "noalloc.cu", "selftest.cu", "paged_append.cu", "paged_attention.cu",
+           "paged_attention_tc.cu", "verify_draft.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "--extended-lambda", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
 

@@ -5,7 +5,7 @@
 #include <string.h>
 
 // Status codes the kernels of the paged cache leave in the word of t5_kernel_status_word (first one wins)
-enum { PAGED_BAD_APPEND = 201, PAGED_BAD_PAGE = 202, PAGED_BAD_LENGTH = 203 };
+enum { PAGED_BAD_APPEND = 201, PAGED_BAD_PAGE = 202, PAGED_BAD_LENGTH = 203, PAGED_TIMEOUT = 204 };
 
 __device__ __forceinline__ void paged_report(int* status, int code) {
   if (status != nullptr) atomicCAS(status, 0, code);
@@ -81,3 +81,5 @@ struct PagedAttnArgs {
 };
 int64_t paged_attention_workspace(int n_rows, int n_q, int H, int Hkv, int d_kv);
 cudaError_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st);
+bool paged_attention_tc_fits(const PagedAttnArgs& a);      // many query rows per kv head, of a form that kernel takes
+cudaError_t launch_paged_attention_tc(const PagedAttnArgs& a, cudaStream_t st);

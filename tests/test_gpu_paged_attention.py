@@ -90,6 +90,100 @@ def test_matches_plain_form(dtype, seq_lens, n_q, h, g, d, page, n_bias, layout,
     check(q, kp, vp, widened(table, page) if wide else table, lens, d ** -0.5, n_q, bias)
 
 
+@pytest.mark.parametrize("n_q,h,g,d", [(17, 1, 1, 64), (5, 32, 4, 128), (8, 16, 4, 128), (3, 24, 4, 64), (11, 6, 1, 64), (8, 8, 1, 64),
+                                       (64, 2, 1, 128), (64, 3, 1, 64), (9, 15, 1, 128), (33, 4, 4, 128), (20, 2, 2, 32)])
+@pytest.mark.parametrize("seq_lens,page,n_bias,layout", [([300, 0, 64, 65, 1000, 1], 16, 32, "slots"), ([5001], 24, 0, "heads"),
+                                                         ([63, 129, 128, 0, 0, 2, 700] * 6, 100, 500, "mixed"),
+                                                         ([200, 17], 1, 1, "slots")])
+def test_many_rows_per_kv_head(n_q, h, g, d, seq_lens, page, n_bias, layout):
+    rng = np.random.default_rng(23)
+    q, kp, vp, table, lens, bias = build(rng, seq_lens, n_q, h, g, d, page, BF16, layout=layout, n_bias=n_bias)
+    table = widened(table, page)
+    check(q, kp, vp, table, lens, 0.125, n_q, bias)
+    lens = rng.integers(-1, max(seq_lens) + 1, len(lens)).tolist()      # rows of a sequence in no order, some empty
+    lens = [min(n, seq_lens[i // n_q]) for i, n in enumerate(lens)]
+    check(q, kp, vp, table, lens, 0.125, n_q, bias)
+
+
+def test_many_rows_agree_bit_for_bit_and_replay_from_a_graph():
+    rng = np.random.default_rng(24)
+    q, kp, vp, table, lens, bias = build(rng, [9000, 200, 0, 77], 5, 16, 2, 128, 16, BF16, n_bias=128)
+    table = widened(table, 16)
+    ws = workspace(20, 5, 16, 2, 128)
+    first, lse = attend(q, kp, vp, table, lens, 0.1, 5, bias, ws)
+    out, lens_d = torch.empty_like(q), i32(lens)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        Bd.t5_paged_attention(q, kp, vp, table, lens_d, out, ws, scale=0.1, n_q=5, bias=bias)
+    for _ in range(20):
+        out.fill_(float("nan"))
+        graph.replay()
+        assert torch.equal(out, first)
+    q.mul_(0.5)
+    graph.replay()
+    assert torch.equal(out, attend(q, kp, vp, table, lens, 0.1, 5, bias, ws)[0]) and not torch.equal(out, first)
+
+
+@pytest.mark.parametrize("n_q,h,g,d", [(5, 16, 2, 128), (8, 8, 2, 64), (20, 8, 1, 128)])
+def test_many_rows_of_sharp_and_large_scores(n_q, h, g, d):
+    rng = np.random.default_rng(25)
+    q, kp, vp, table, lens, _ = build(rng, [700, 129, 64], n_q, h, g, d, 16, BF16, spread=30.0)
+    check(q, kp, vp, widened(table, 16), lens, 1.0, n_q, None)
+
+
+@pytest.mark.parametrize("n_q,h,g,d", [(6, 12, 3, 64), (10, 5, 1, 128), (30, 6, 1, 64)])
+def test_many_rows_and_a_bias_that_masks(n_q, h, g, d):
+    """The lowest value on every key of a head leaves a uniform mean, -infinity an empty row."""
+    rng = np.random.default_rng(26)
+    q, kp, vp, table, lens, bias = build(rng, [200, 70, 6], n_q, h, g, d, 16, BF16, n_bias=8)
+    bias[1], bias[2] = torch.finfo(F32).min, -float("inf")
+    out, lse = attend(q, kp, vp, widened(table, 16), lens, 0.1, n_q, bias)
+    ref, rlse, tol, ltol = SR.attention(q, kp, vp, table, lens, 16, n_q, 0.1, bias)
+    others = [i for i in range(h) if i not in (1, 2)]
+    assert bool(((out.double() - ref).abs() <= tol)[:, others].all())
+    assert not out[:, 2].any() and bool((lse[:, 2] == -float("inf")).all())
+    for r, n in enumerate(lens):
+        pg, sl = SR.slots_of(table, r // n_q, n, 16)
+        v = vp[pg, sl][:, 1 // (h // g)].double()
+        want = v.mean(0) if n else torch.zeros(d, device=DEV)
+        assert (out[r, 1].double() - want).abs().max() <= (SR.HALF[BF16] + 2.0 ** -15) * (v.abs().max() if n else 1)
+
+
+def test_many_rows_and_pages_that_are_none():
+    rng = np.random.default_rng(27)
+    n_q, h, g, d = 5, 10, 2, 128
+    q, kp, vp, table, _, _ = build(rng, [330], n_q, h, g, d, 24, BF16)
+    good, table = table.clone(), widened(table, 24)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    Bd.t5_kernel_status_word(status)
+    try:
+        attend(q, kp, vp, table, [300] * n_q, 0.1, n_q, None)
+        assert status.item() == 0
+        table[0, 1], table[0, 6], table[0, 7] = kp.shape[0], -1, -2 ** 31
+        out, _ = attend(q, kp, vp, table, [300] * n_q, 0.1, n_q, None)
+        assert status.item() == 202
+    finally:
+        Bd.t5_kernel_status_word(None)
+    keep = [j for j in range(300) if j // 24 not in (1, 6, 7)]
+    pg, sl = SR.slots_of(good, 0, 300, 24)
+    k, v = (x[pg, sl][keep].double().repeat_interleave(h // g, 1) for x in (kp, vp))
+    w = torch.softmax(torch.einsum("nhd,rhd->rhn", k, q.double()) * 0.1, -1)
+    ref = torch.einsum("rhn,nhd->rhd", w, v)
+    assert (out.double() - ref).abs().max() <= (SR.HALF[BF16] + 2.0 ** -12) * v.abs().max()
+
+
+def test_many_rows_of_a_cache_beyond_four_gigabytes():
+    n_pages, page, g, d, n_q = 4200, 64, 64, 128, 20
+    kp = torch.empty(n_pages, page, g, d, dtype=BF16, device=DEV)
+    vp = torch.empty_like(kp)
+    table = i32([[n_pages - 1, 0, n_pages - 2]])
+    for p in table[0].tolist():
+        kp[p], vp[p] = torch.randn(page, g, d, device=DEV).to(BF16), torch.randn(page, g, d, device=DEV).to(BF16)
+    q = torch.randn(n_q, g, d, device=DEV).to(BF16)
+    check(q, kp, vp, widened(table, 64), [150 - i for i in range(n_q)], 0.09, n_q, None)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_many_sequences_of_every_length(dtype):
     """More sequences than threads look at at once, in no order of length, many of them empty."""
