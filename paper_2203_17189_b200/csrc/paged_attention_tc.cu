@@ -167,53 +167,61 @@ paged_attn_tc_kernel(const __grid_constant__ AttnParams a, const __grid_constant
     const int boxes = kTile >> box_log2, box = 1 << box_log2;
     const uint32_t lead = elect_one_lane();
     auto look = [&]() { return lane < boxes ? page_entry(a, cur, cur.blk * kTile + lane * box) : kNoKey; };
-    int entry = n > 0 ? look() : kNoKey, t = 0;
-    bool k_out = false;      // keys of tile t are on their way, its values not
-    for (; t < n; ++t) {
-      const int st = t & 1, first_key = cur.blk * kTile, key = first_key + lane * box, keys = cur.len - first_key;
-      const int slot = lane < boxes ? key - (int)a.pool.ps.div(key) * a.pool.page_size : 0;
-      const int page = page_of(a, entry), at = page < 0 ? a.pool.n_pages : page, head = (int)a.by_tiles.div(cur.k);
-      const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
-      const uint32_t low = __ballot_sync(0xffffffffu, ((there >> (lane >> box_log2)) & 1) && lane < keys);
-      const uint32_t high = __ballot_sync(0xffffffffu, ((there >> ((lane + 32) >> box_log2)) & 1) && lane + 32 < keys);
-      step(a, kTile, cur);
-      if (t + 1 < n) entry = look();
-      int pages[kTile / 8], slots[kTile / 8];      // of all boxes: one lane issues them, lanes of a warp would only take turns
+    struct Boxes { int page[kTile / 8], slot[kTile / 8], head; };      // of a tile
+    auto load = [&](const CUtensorMap* map, const Boxes& x, int to, uint64_t* full) {
+      if (lead) {      // one lane for all boxes: lanes of a warp would only take turns
+        mbar_arrive_expect_tx(full, L::KV_BYTES);
 #pragma unroll
-      for (int i = 0; i < kTile / 8; ++i) {
-        pages[i] = __shfl_sync(0xffffffffu, at, i);
-        slots[i] = __shfl_sync(0xffffffffu, slot, i);
-      }
-      auto load = [&](const CUtensorMap* map, int to, uint64_t* full) {
-        if (lead) {
-          mbar_arrive_expect_tx(full, L::KV_BYTES);
+        for (int i = 0; i < kTile / 8; ++i) {
+          if (i == boxes) break;
 #pragma unroll
-          for (int i = 0; i < kTile / 8; ++i) {
-            if (i == boxes) break;
-#pragma unroll
-            for (int c = 0; c < DK / 64; ++c)
-              tma_load_4d(smem + to + c * (kTile * 128) + i * box * 128, map, c * 64, head, slots[i], pages[i], full);
-          }
+          for (int c = 0; c < DK / 64; ++c)
+            tma_load_4d(smem + to + c * (kTile * 128) + i * box * 128, map, c * 64, x.head, x.slot[i], x.page[i], full);
         }
-        __syncwarp();
-      };
-      if (t >= 2 && !wait(&ms->free_k[st], ((t >> 1) - 1) & 1)) break;
-      if (lead) { ms->ok[t % kRing][0] = low; ms->ok[t % kRing][1] = high; }
-      load(&k_map, L::K + st * L::KV_BYTES, &ms->full_k[st]);
-      k_out = true;
-      if (t >= 2 && !wait(&ms->free_v[st], ((t >> 1) - 1) & 1)) break;
-      load(&v_map, L::V + st * L::KV_BYTES, &ms->full_v[st]);
-      k_out = false;
+      }
+      __syncwarp();
+    };
+    int entry = n > 0 ? look() : kNoKey, out_k = 0, out_v = 0;      // out_*: tiles sent for
+    Boxes now = {}, last;
+    // Keys go a tile ahead of the values, as scores do of outputs: sent for together, the keys of a tile waited for the
+    // output of the one three before it (24 rows, 64 sequences of up to 8192 keys: 126 instead of 120 us)
+    for (int t = 0; t <= n && n > 0; ++t) {
+      last = now;
+      if (t < n) {
+        const int first_key = cur.blk * kTile, key = first_key + lane * box, keys = cur.len - first_key;
+        const int slot = lane < boxes ? key - (int)a.pool.ps.div(key) * a.pool.page_size : 0;
+        const int page = page_of(a, entry), at = page < 0 ? a.pool.n_pages : page;
+        const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
+        const uint32_t low = __ballot_sync(0xffffffffu, ((there >> (lane >> box_log2)) & 1) && lane < keys);
+        const uint32_t high = __ballot_sync(0xffffffffu, ((there >> ((lane + 32) >> box_log2)) & 1) && lane + 32 < keys);
+        now.head = (int)a.by_tiles.div(cur.k);
+        step(a, kTile, cur);
+        if (t + 1 < n) entry = look();
+#pragma unroll
+        for (int i = 0; i < kTile / 8; ++i) {
+          now.page[i] = __shfl_sync(0xffffffffu, at, i);
+          now.slot[i] = __shfl_sync(0xffffffffu, slot, i);
+        }
+        if (t >= 2 && !wait(&ms->free_k[t & 1], ((t >> 1) - 1) & 1)) break;
+        if (lead) { ms->ok[t % kRing][0] = low; ms->ok[t % kRing][1] = high; }
+        load(&k_map, now, L::K + (t & 1) * L::KV_BYTES, &ms->full_k[t & 1]);
+        out_k = t + 1;
+      }
+      if (t >= 1) {
+        const int v = t - 1;
+        if (v >= 2 && !wait(&ms->free_v[v & 1], ((v >> 1) - 1) & 1)) break;
+        load(&v_map, last, L::V + (v & 1) * L::KV_BYTES, &ms->full_v[v & 1]);
+        out_v = t;
+      }
     }
     // no copy may be on its way when the CTA ends (with a limit, should a wait above have given up)
     const long long t0 = clock64();
     auto landed = [&](uint64_t* full, int tile) {
       while (!mbar_try_wait(&full[tile & 1], (tile >> 1) & 1) && clock64() - t0 < kWaitCycles) {}
     };
-    const int last_v = t - 1, last_k = k_out ? t : last_v;
-    for (int i = 0; i < 2; ++i) {
-      if (last_k - i >= 0) landed(ms->full_k, last_k - i);
-      if (last_v - i >= 0) landed(ms->full_v, last_v - i);
+    for (int i = 1; i <= 2; ++i) {
+      if (out_k >= i) landed(ms->full_k, out_k - i);
+      if (out_v >= i) landed(ms->full_v, out_v - i);
     }
   } else if (w == kMmaWarp) {
     // ------------------------------------------------------------ products
@@ -544,7 +552,7 @@ cudaError_t run_rows(AttnParams& a, const CUtensorMap& k, const CUtensorMap& v, 
 
 // More rows than one tile of the kernels for few, and, for two tiles of those, caches that may be long: an item costs more
 // here and a tile less.  Measured, us there / here, 32 rows over 8 kv heads of 128 columns: 128 sequences of up to 300 keys
-// 59 / 72, 32 of up to 1000 44 / 40; 4 kv heads, 64 sequences of up to 8192 183 / 127; 40 rows, up to 300 keys 53 / 50, up to
+// 59 / 72, 32 of up to 1000 44 / 40; 4 kv heads, 64 sequences of up to 8192 183 / 120; 40 rows, up to 300 keys 53 / 50, up to
 // 8192 261 / 148.
 bool paged_attention_tc_fits(const PagedAttnArgs& g) {
   const int64_t limit = 1ll << 40;      // of a tensor's strides
