@@ -249,18 +249,15 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t&
 __device__ __forceinline__ bool not_finite(uint32_t two) {      // either bfloat16 has an exponent of all ones
   return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
 }
-// Joins the pieces of the item that the boundary behind CTA blockIdx.x is the first to cut; one CTA per boundary and query
-// row.  Its warps take every kJoinWarps-th piece, eight at a time with all their loads on the way at once, and combine what
-// they have in shared memory (74 pieces of an item, one sequence of 46,900 keys: 11 us with separate passes for maxima, sums
-// and columns, 7 us so).  SPLIT = false, for many rows of few pieces: a warp per row (64 rows at 295 boundaries: a CTA per row
-// took 28 us).
+// Joins the pieces of the item that the boundary behind CTA blockIdx.x is the first to cut, kJoinWarps query rows in a CTA.
+// Up to eight pieces: a warp per row (a CTA per row took 28 us for 64 rows at 295 boundaries, 9 us for 8).  More: the warps
+// take every kJoinWarps-th piece of a row, eight at a time with all their loads on the way at once, and combine what they have
+// in shared memory (74 pieces, one sequence of 46,900 keys: 11 us with separate passes for maxima, sums and columns, 7 us so).
 constexpr int kJoinWarps = 4;
-template <typename T, int DK, int RT, bool SPLIT>
+template <typename T, int DK, int RT>
 __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const __grid_constant__ AttnParams a, int ctas) {
   pdl_sync();
-  constexpr int STEP = SPLIT ? kJoinWarps : 1;      // warps that share a row's pieces
-  const int tid = threadIdx.x, lane = tid & 31, w = SPLIT ? tid >> 5 : 0;
-  const int c0 = blockIdx.x, r = SPLIT ? (int)blockIdx.y : (int)blockIdx.y * kJoinWarps + (tid >> 5);
+  const int c0 = blockIdx.x, r0 = blockIdx.y * kJoinWarps, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int item = a.meta[c0].z;
   // pieces: slot 1 of c0, then slot 0 of the CTAs behind it up to the one where the item ends (a CTA without work lies
   // between items, never inside one)
@@ -274,53 +271,61 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
   }
   const Place p = item_place(a, item);
   const Rows rows(a, p, RT);
-  if (r >= rows.n) return;
   const int n = last - c0 + 1;
   constexpr int VC = DK / 32;
   struct alignas(VC * 4) Cols { float v[VC]; };
-  float mx = -INFINITY, sum = 0.f, acc[VC];
+  // pieces i0, i0 + by, ... of row r: their maximum, and sum and columns relative to it
+  auto gather = [&](int r, int i0, int by, float& mx, float& sum, float (&acc)[VC]) {
+    mx = -INFINITY; sum = 0.f;
 #pragma unroll
-  for (int c = 0; c < VC; ++c) acc[c] = 0.f;
-  for (int i0 = w; i0 < n; i0 += 8 * STEP) {
-    float2 ms[8];      // maximum and sum
-    Cols v[8];
-    float top = mx;
+    for (int c = 0; c < VC; ++c) acc[c] = 0.f;
+    for (; i0 < n; i0 += 8 * by) {
+      float2 ms[8];      // maximum and sum
+      Cols v[8];
+      float top = mx;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int i = i0 + k * STEP;
-      ms[k] = make_float2(-INFINITY, 0.f);
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * by;
+        ms[k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-      for (int c = 0; c < VC; ++c) v[k].v[c] = 0.f;
-      if (i < n) {
-        const float* q = a.part + (((int64_t)(c0 + i) * 2 + (i == 0 ? 1 : 0)) * a.rows + r) * kRowOf<DK>;
-        ms[k] = *reinterpret_cast<const float2*>(q + DK);
-        v[k] = *reinterpret_cast<const Cols*>(q + lane * VC);
+        for (int c = 0; c < VC; ++c) v[k].v[c] = 0.f;
+        if (i < n) {
+          const float* q = a.part + (((int64_t)(c0 + i) * 2 + (i == 0 ? 1 : 0)) * a.rows + r) * kRowOf<DK>;
+          ms[k] = *reinterpret_cast<const float2*>(q + DK);
+          v[k] = *reinterpret_cast<const Cols*>(q + lane * VC);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top = fmaxf(top, ms[k].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+      const float f = ex2((mx - ref) * kLog2e);
+      mx = top;
+      sum *= f;
+#pragma unroll
+      for (int c = 0; c < VC; ++c) acc[c] *= f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float e = ex2((ms[k].x - ref) * kLog2e);
+        sum += e * ms[k].y;
+#pragma unroll
+        for (int c = 0; c < VC; ++c) acc[c] += e * v[k].v[c];
       }
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) top = fmaxf(top, ms[k].x);
-    const float ref = top == -INFINITY ? 0.f : top;
-    const float f = ex2((mx - ref) * kLog2e);
-    mx = top;
-    sum *= f;
-#pragma unroll
-    for (int c = 0; c < VC; ++c) acc[c] *= f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float e = ex2((ms[k].x - ref) * kLog2e);
-      sum += e * ms[k].y;
-#pragma unroll
-      for (int c = 0; c < VC; ++c) acc[c] += e * v[k].v[c];
-    }
-  }
-  if constexpr (!SPLIT) {
-    int row, h;
-    rows.place(a, p, r, row, h);
+  };
+  float mx, sum, acc[VC];
+  int row, h;
+  if (n <= 8) {
+    if (r0 + w >= rows.n) return;
+    gather(r0 + w, 0, 1, mx, sum, acc);
+    rows.place(a, p, r0 + w, row, h);
 #pragma unroll
     for (int c = 0; c < VC; ++c) out_row<T, DK>(a, row, h)[lane * VC + c] = from_f<T>(sum == 0.f ? 0.f : acc[c] / sum);
     if (lane == 0) write_lse(a, row, h, mx, sum);
-  } else {
-    __shared__ float red[kJoinWarps][DK], red_m[kJoinWarps], red_s[kJoinWarps];
+    return;
+  }
+  __shared__ float red[kJoinWarps][DK], red_m[kJoinWarps], red_s[kJoinWarps];
+  for (int r = r0; r < min(r0 + kJoinWarps, rows.n); ++r) {
+    gather(r, w, kJoinWarps, mx, sum, acc);
 #pragma unroll
     for (int c = 0; c < VC; ++c) red[w][lane * VC + c] = acc[c];
     if (lane == 0) { red_m[w] = mx; red_s[w] = sum; }
@@ -338,11 +343,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attn_join_kernel(const 
         out += e * red[i][tid];
         sum += e * red_s[i];
       }
-      int row, h;
       rows.place(a, p, r, row, h);
       out_row<T, DK>(a, row, h)[tid] = from_f<T>(sum == 0.f ? 0.f : out / sum);
       if (tid == 0) write_lse(a, row, h, mx, sum);
     }
+    __syncthreads();
   }
 }
 
@@ -393,6 +398,10 @@ cudaError_t grid_of(Kernel kernel, int smem, int* ctas) {
   *ctas = n;
   return cudaSuccess;
 }
+template <typename T, int DK, int RT> cudaError_t launch_join(const AttnParams& a, int ctas, cudaStream_t st) {
+  return launch_pdl(paged_attn_join_kernel<T, DK, RT>, dim3(ctas - 1, (a.rows + kJoinWarps - 1) / kJoinWarps),
+                    dim3(kJoinWarps * 32), 0, st, a, ctas);
+}
 // The kernel over equal shares of the line, and the one that joins what it cut
 template <typename T, int DK, int RT>
 cudaError_t launch_line(AttnParams& a, Kernel line, int smem, cudaStream_t st) {
@@ -403,7 +412,7 @@ cudaError_t launch_line(AttnParams& a, Kernel line, int smem, cudaStream_t st) {
   a.extra = a.bias != nullptr ? 2 : 1;
   e = launch_pdl(line, dim3(ctas), dim3(kThreads), (size_t)smem, st, a);
   if (e != cudaSuccess) return e;
-  return launch_pdl(paged_attn_join_kernel<T, DK, RT, true>, dim3(ctas - 1, a.rows), dim3(kJoinWarps * 32), 0, st, a, ctas);
+  return launch_join<T, DK, RT>(a, ctas, st);
 }
 
 }  // namespace

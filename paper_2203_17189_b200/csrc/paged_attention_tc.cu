@@ -538,8 +538,7 @@ cudaError_t run(AttnParams& a, const CUtensorMap& k_map, const CUtensorMap& v_ma
   a.extra = a.bias != nullptr ? 2 : 1;
   e = launch_pdl(paged_attn_tc_kernel<DK, R>, dim3(ctas), dim3(kTcThreads), (size_t)smem, st, a, k_map, v_map, box_log2);
   if (e != cudaSuccess) return e;
-  return launch_pdl(paged_attn_join_kernel<bf16, DK, R, false>, dim3(ctas - 1, (a.rows + kJoinWarps - 1) / kJoinWarps),
-                    dim3(kJoinWarps * 32), 0, st, a, ctas);
+  return launch_join<bf16, DK, R>(a, ctas, st);
 }
 template <int DK>
 cudaError_t run_rows(AttnParams& a, const CUtensorMap& k, const CUtensorMap& v, int box_log2, cudaStream_t st) {
