@@ -21,7 +21,6 @@
 #include <cooperative_groups.h>
 #include <math.h>
 #include <string.h>
-#include <utility>
 
 namespace cg = cooperative_groups;
 
@@ -138,7 +137,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
   const int K = a.K, V = a.V;
   const int n = a.n_draft != nullptr ? min(max(a.n_draft[s], 0), K) : K;
   const double u = fmax((double)a.u_sample[s], 0.0);      // below 0 and NaN: 0, so that what it draws has mass
-  auto started = cluster.barrier_arrive();      // waited for where the CTAs first write to each other
+  if (cs > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;");      // "has started", waited for below
   if (tid == 0) { first = K; run_at = -1; }
   __syncthreads();
   const T* tgt = reinterpret_cast<const T*>(a.target) + s * a.t_seq;
@@ -171,7 +170,8 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
     const int skip = attempt == 0 ? hole : -1;
     if (d != nullptr) sum_runs<T, LN, true>(tr, d, r0, r1 - r0, V, a.vec, skip, runs);
     else sum_runs<T, LN, false>(tr, d, r0, r1 - r0, V, a.vec, skip, runs);
-    if (attempt == 0) cluster.barrier_wait(std::move(started));
+    // CTAs write to each other next: all have to have started
+    if (attempt == 0 && cs > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     __syncthreads();
     // inclusive prefix sums of the runs
     if (w == 0) {
@@ -188,7 +188,8 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
       }
       if (lane < cs) *cluster.map_shared_rank(&totals[attempt][rank], lane) = carry;
     }
-    cluster.sync();
+    if (cs > 1) cluster.sync();
+    else __syncthreads();
     double before = 0.0, total = 0.0;
     int last = -1;      // the last CTA with any mass
     for (int c = 0; c < cs; ++c) {
