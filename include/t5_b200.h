@@ -400,7 +400,8 @@ T5_API int t5_attention_backward_noalloc(
  *  - max_pages * page_size <= 2^30 positions per sequence.
  *  - What the host cannot check is checked on the device and reported through t5_kernel_status_word: 201 = a token to
  *    append has no place (sequence, position or page out of range; it is left out), 202 = a page in front of a length is
- *    out of range (its keys count as absent), 203 = a length beyond max_pages * page_size (cut to that). */
+ *    out of range (its keys count as absent), 203 = a length beyond max_pages * page_size (cut to that).  204 = a bounded
+ *    wait inside the attention kernel ran out (its result is not valid). */
 
 /* Appends n_tokens new keys and values: token t, heads in columns [g * d_kv, (g + 1) * d_kv) of row t of d_k / d_v (row
  * strides ldk, ldv), goes to position d_positions[t] of sequence d_seq[t] (0 .. n_seqs - 1).  A negative position is
